@@ -280,6 +280,86 @@ skim_status skim_dequant_matvec_f32(skim_ctx *ctx, const uint32_t *codes, const 
                                     const int32_t *row_perm, const uint16_t *codebooks_fp16,
                                     const float *alpha, int64_t n, int64_t m, const float *x, float *y);
 
+/* ---- 4-bit weights with group scales ---------------------------------------- */
+
+/* Element types of activations and results.  SKIM_E4M3: 8-bit floats of 4 exponent and 3 mantissa bits, largest number 448,
+ * no infinities (torch.float8_e4m3fn). */
+typedef enum { SKIM_F32 = 0, SKIM_BF16 = 1, SKIM_E4M3 = 2 } skim_dtype;
+
+/* A uniform alternative to the codebooks of skim_pack, for layers that are used in products with many tokens, and to compare
+ * with: every group of `group` neighbouring columns of a row (32, 64 or 128; the last one as long as the row has columns) has one
+ * scale s, every weight is s q with a whole number q in -7..7,
+ *   s = the least number of 5 significant bits that is not below max |w| / 7, and at least 2^-126 (0 for a group of zeros),
+ *   q = w / s rounded to the nearest whole number, ties to even:     |w - s q| <= s / 2.
+ * s q has at most 8 significant bits and so is a bfloat16 exactly: the products below read the quantised matrix without rounding it again.
+ *
+ * codes: skim_group_code_words(n, m) uint32, 16-byte aligned.  Blocks of 16 rows x 128 columns, 1 KB each, block (i, j) at word
+ *   (i ceil(m / 128) + j) 256; in it word 4 (16 c + r) + k holds row r, columns 32 k + 8 c + 0..7 of the block (c, k in 0..3).  In a word
+ *   the size of column b (b = 0..3) is in bits 8 b .. 8 b + 2, its sign in bit 8 b + 7; the size of column 4 + b is in bits 8 b + 4 .. 8 b + 6,
+ *   its sign in bit 8 ((b + 1) mod 4) + 3.  Rows and columns past the matrix, up to whole blocks, hold 0.
+ * scales: skim_group_scale_entries(n, m, group) bfloat16, 16-byte aligned: [128 / group x ceil(m / 128)][16 ceil(n / 16)], group by group,
+ *   0 past the matrix.
+ * The sizes are -1 for arguments that the calls reject.  n, m <= SKIM_GROUP_MAX, fewer than 2^31 blocks.
+ *
+ * skim_group_quantize: W dev, n x m float32, stride ld; finite, and below 2^127 in size.
+ * skim_group_unpack: Wq dev float32 n x m, stride m. */
+#define SKIM_GROUP_MAX (1 << 24)
+int64_t skim_group_code_words(int64_t n, int64_t m);
+int64_t skim_group_scale_entries(int64_t n, int64_t m, int group);
+skim_status skim_group_quantize(skim_ctx *ctx, const float *W, int64_t n, int64_t m, int64_t ld, int group, uint32_t *codes,
+                                uint16_t *scales_bf16);
+skim_status skim_group_unpack(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group, float *Wq);
+
+/* Products with such a matrix W, for T tokens (T = 0: nothing is done).
+ *   skim_group_matmul:     y = x W^T         x: T x m, y: T x n
+ *   skim_group_matmul_dx:  dx = dy W         dy: T x n, dx: T x m   (the gradient to x; W is fixed)
+ * x: dev, SKIM_BF16 with x_scales NULL, or SKIM_E4M3 with x_scales dev float32[T]: token t is x_scales[t] times its row of x (what
+ * skim_rms_norm writes).  Row strides ldx >= m, lddy >= n in elements; any alignment, but rows on 16-byte borders (8-byte ones for
+ * e4m3) whose length is a multiple of 8 are read faster.  Results: SKIM_BF16 or SKIM_F32, dense, apart from all inputs.
+ * Operands are exact and sums float32; a result is rounded once, to its type.  What x holds behind a row's m columns is not used. */
+skim_status skim_group_matmul(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
+                              const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, void *y, int y_type);
+skim_status skim_group_matmul_dx(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
+                                 const uint16_t *dy_bf16, int64_t lddy, int64_t T, void *dx, int dx_type);
+
+/* The gated half of a feed-forward block, both projections, the activation and the product in one pass:
+ *   a = silu(x Wg^T) * (x Wu^T),   silu(g) = g / (1 + exp(-g))
+ * with two n x m matrices of the same group.  x as above; a: dev T x n, dense, SKIM_BF16 or SKIM_F32 (rounded once).
+ * The backward pass, with fixed matrices, works g = x Wg^T and u = x Wu^T out again (so x is all that has to be kept, 8 bits of it will do):
+ *   dgate = da u silu'(g),  dup = da silu(g)      dev T x n bfloat16, dense, 16-byte aligned
+ *   dx = dgate Wg + dup Wu                        dev T x m, dense, SKIM_BF16 or SKIM_F32; NULL = not wanted
+ * da: dev T x n bfloat16, row stride ldda >= n.  dx is made of dgate and dup as they are stored.  For x in e4m3 dx is the gradient to
+ * the token's row times its scale. */
+skim_status skim_group_glu(skim_ctx *ctx, const uint32_t *gate_codes, const uint16_t *gate_scales, const uint32_t *up_codes,
+                           const uint16_t *up_scales, int64_t n, int64_t m, int group, const void *x, int x_type, int64_t ldx,
+                           const float *x_scales, int64_t T, void *a, int a_type);
+skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *gate_codes, const uint16_t *gate_scales, const uint32_t *up_codes,
+                                    const uint16_t *up_scales, int64_t n, int64_t m, int group, const void *x, int x_type, int64_t ldx,
+                                    const float *x_scales, int64_t T, const uint16_t *da_bf16, int64_t ldda, uint16_t *dgate_bf16,
+                                    uint16_t *dup_bf16, void *dx, int dx_type);
+
+/* Root-mean-square norm, with the residual's addition ahead of it and an 8-bit output for the products above:
+ *   h = x + residual (rounded to the type; without a residual h is x),  rstd = 1 / sqrt(mean_j h_j^2 + eps),  y_j = h_j rstd weight_j
+ *   scales = max_j |y_j| / 448 (float32, at least 2^-126; 1 for a row of zeros),   q_j = y_j / scales rounded to e4m3, ties to even
+ * Statistics and the quotients are float64: q is the rounding of the formula's value.
+ * x, residual: dev rows x m of `type` (SKIM_BF16 or SKIM_F32), row strides ldx, ldr >= m.  weight: dev float32[m], NULL = 1.
+ * h (given with residual and only then; it may be x or residual itself where that is dense), y: dev rows x m of `type`, dense; q: dev
+ * rows x m bytes with scales dev float32[rows]; rstd: dev float32[rows].  y, q with scales, and rstd may be NULL, not all of them.
+ * eps > 0, 1 <= m <= SKIM_MAX_M. */
+skim_status skim_rms_norm(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, int type, const float *weight,
+                          float eps, int64_t rows, int64_t m, void *h, void *y, uint8_t *q_e4m3, float *scales, float *rstd);
+
+/* Its backward pass, through y (the rounding to 8 bits passes gradients on unchanged):
+ *   with n = h rstd and g = dy weight:   dx = rstd (g - n mean_j(g_j n_j)) + dh,   dweight = sum over the rows of dy n
+ * dy: dev rows x m of `type`: the gradient to y; h: what skim_rms_norm wrote (x where there was no residual), rstd likewise; dh: the
+ * gradient that reaches h past the norm, NULL = none; row strides lddy, ldh, lddh.  dx: dev rows x m of `type`, dense: the gradient to x, and
+ * to the residual.  dweight: dev float32[m], NULL = not wanted; it needs scratch (dev, 4-byte aligned) of
+ * skim_rms_norm_scratch_bytes(ctx, rows, m) bytes.  Arithmetic in float32, the rows of dweight added in a fixed order. */
+size_t skim_rms_norm_scratch_bytes(const skim_ctx *ctx, int64_t rows, int64_t m);
+skim_status skim_rms_norm_backward(skim_ctx *ctx, const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dh, int64_t lddh,
+                                   int type, const float *rstd, const float *weight, int64_t rows, int64_t m, void *dx, float *dweight,
+                                   void *scratch, size_t scratch_bytes);
+
 /* ---- scaling vector ----------------------------------------------------- */
 
 /* Layer-wise Hessian proxy from calibration activations (Sec. 3.4):

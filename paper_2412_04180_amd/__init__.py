@@ -20,12 +20,16 @@ STATUS_NAMES = {0: "SKIM_OK", -1: "SKIM_ERR_ARG", -2: "SKIM_ERR_SHAPE", -3: "SKI
                 -4: "SKIM_ERR_WORKSPACE", -5: "SKIM_ERR_HIP", -6: "SKIM_ERR_NONFINITE"}
 MAX_M = 32768
 PACK_STATIC_MAX_ROWS = 65536
+GROUP_MAX = 1 << 24
+F32, BF16, E4M3 = 0, 1, 2          # skim_dtype
 
 EXPORTS = ["skim_create", "skim_destroy", "skim_last_error", "skim_workspace_bytes", "skim_set_workspace",
            "skim_profile_enable", "skim_profile_last", "skim_validate_enable",
            "skim_error_table", "skim_error_table_lfull", "skim_cluster_rows", "skim_select_allocated", "skim_greedy_allocate", "skim_greedy_allocate_device",
            "skim_dp_allocate_scratch_bytes", "skim_dp_allocate", "skim_kmeans_optimal_scratch_bytes", "skim_kmeans_optimal",
-           "skim_packed_words", "skim_codebook_entries", "skim_pack", "skim_pack_static", "skim_layer_loss", "skim_scale_step", "skim_train_scale", "skim_unpack", "skim_dequant_matvec", "skim_dequant_matvec_f32", "skim_hessian_workspace_bytes", "skim_hessian_from_activations", "skim_hessian_from_activations_scratch"]
+           "skim_packed_words", "skim_codebook_entries", "skim_pack", "skim_pack_static", "skim_layer_loss", "skim_scale_step", "skim_train_scale", "skim_unpack", "skim_dequant_matvec", "skim_dequant_matvec_f32", "skim_group_code_words", "skim_group_scale_entries", "skim_group_quantize", "skim_group_unpack", "skim_group_matmul", "skim_group_matmul_dx",
+           "skim_group_glu", "skim_group_glu_backward", "skim_rms_norm", "skim_rms_norm_scratch_bytes", "skim_rms_norm_backward",
+           "skim_hessian_workspace_bytes", "skim_hessian_from_activations", "skim_hessian_from_activations_scratch"]
 
 
 class SkimError(RuntimeError):
@@ -92,6 +96,20 @@ def load_library():
         lib.skim_unpack.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, vp]
         lib.skim_dequant_matvec.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, vp, vp]
         lib.skim_dequant_matvec_f32.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, vp, vp]
+        lib.skim_group_code_words.argtypes = [i64, i64]
+        lib.skim_group_code_words.restype = i64
+        lib.skim_group_scale_entries.argtypes = [i64, i64, i32]
+        lib.skim_group_scale_entries.restype = i64
+        lib.skim_group_quantize.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp]
+        lib.skim_group_unpack.argtypes = [vp, vp, vp, i64, i64, i32, vp]
+        lib.skim_group_matmul.argtypes = [vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32]
+        lib.skim_group_matmul_dx.argtypes = [vp, vp, vp, i64, i64, i32, vp, i64, i64, vp, i32]
+        lib.skim_group_glu.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32]
+        lib.skim_group_glu_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i64, vp, vp, vp, i32]
+        lib.skim_rms_norm.argtypes = [vp, vp, i64, vp, i64, i32, vp, C.c_float, i64, i64, vp, vp, vp, vp, vp]
+        lib.skim_rms_norm_scratch_bytes.argtypes = [vp, i64, i64]
+        lib.skim_rms_norm_scratch_bytes.restype = C.c_size_t
+        lib.skim_rms_norm_backward.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, vp, vp, i64, i64, vp, vp, vp, C.c_size_t]
         lib.skim_train_scale.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, i32, i32, i32, i64, C.POINTER(AdamOpts),
                                          vp, vp, vp, vp, vp, vp]
         _lib = lib
@@ -412,6 +430,171 @@ class Context:
                                                      _dp(pk["row_perm"]), _dp(pk["codebooks"]), _dp(alpha), n, m,
                                                      _dp(x), _dp(y)))
         return y
+
+    # -- 4-bit weights with group scales --------------------------------------
+    def _rows(self, x, dtypes, columns, what):
+        """(pointer, row stride, rows) of a 2-D device tensor of one of `dtypes`, or of a vector (one row)."""
+        one = x.dim() == 1
+        assert x.dtype in dtypes and x.device == self.device and x.dim() in (1, 2), what
+        assert x.shape[-1] == columns and x.stride(-1) == 1, what
+        rows = 1 if one else x.shape[0]
+        return x.data_ptr(), (columns if one or rows < 2 else x.stride(0)), rows
+
+    def _result(self, out, shape, dtype, what):
+        """`out`, checked, or a new tensor."""
+        if out is None:
+            return self.empty(shape, dtype)
+        assert tuple(out.shape) == tuple(shape) and out.dtype == dtype and out.device == self.device and out.is_contiguous(), what
+        return out
+
+    def _group_pointers(self, gq):
+        codes, scales = gq["codes"], gq["scales"]
+        assert codes.dtype == self.torch.int32 and scales.dtype == self.torch.bfloat16 and codes.is_contiguous() and scales.is_contiguous()
+        assert codes.device == self.device and scales.device == self.device
+        n, m, group = gq["n"], gq["m"], gq["group"]
+        assert codes.numel() == self.lib.skim_group_code_words(n, m) and scales.numel() == self.lib.skim_group_scale_entries(n, m, group)
+        return codes.data_ptr(), scales.data_ptr(), n, m, group
+
+    def _group_input(self, x, x_scales, m, what):
+        """(pointer, type, row stride, pointer of the scales, tokens) of the input of a product."""
+        t = self.torch
+        p, ld, T = self._rows(x, (t.bfloat16, t.float8_e4m3fn), m, what)
+        if x.dtype == t.bfloat16:
+            assert x_scales is None, what + ": scales go with e4m3"
+            return p, BF16, ld, None, T
+        assert x_scales is not None and x_scales.dtype == t.float32 and x_scales.device == self.device and x_scales.is_contiguous(), what
+        assert x_scales.numel() == T, what
+        return p, E4M3, ld, x_scales.data_ptr(), T
+
+    def _result_type(self, out, out_dtype):
+        dtype = out.dtype if out is not None else out_dtype if out_dtype is not None else self.torch.bfloat16
+        assert dtype in (self.torch.bfloat16, self.torch.float32), "results are bfloat16 or float32"
+        return dtype, (BF16 if dtype == self.torch.bfloat16 else F32)
+
+    def group_quantize(self, W, group=128, out=None):
+        """4-bit codes and group scales (skim_group_quantize) of W: float32 device tensor n x m (row stride W.stride(0)).
+        Returns dict(codes, scales, n, m, group), what the products below take."""
+        t = self.torch
+        n, m = W.shape
+        p, ld, _ = self._rows(W, (t.float32,), m, "group_quantize: W")
+        words, entries = int(self.lib.skim_group_code_words(n, m)), int(self.lib.skim_group_scale_entries(n, m, group))
+        if words < 0 or entries < 0:
+            raise ValueError("group_quantize: n, m up to 2^24, groups of 32, 64 or 128 columns")
+        n16 = (n + 15) // 16 * 16
+        codes = self._result(out["codes"] if out else None, (words,), t.int32, "group_quantize: codes")
+        scales = self._result(out["scales"] if out else None, (entries // n16, n16), t.bfloat16, "group_quantize: scales")
+        self._check(self.lib.skim_group_quantize(self.h, p, n, m, ld, group, codes.data_ptr(), scales.data_ptr()))
+        return dict(codes=codes, scales=scales, n=n, m=m, group=group)
+
+    def group_unpack(self, gq, out=None):
+        """Dense float32 n x m matrix of what group_quantize returned."""
+        codes, scales, n, m, group = self._group_pointers(gq)
+        Wq = self._result(out, (n, m), self.torch.float32, "group_unpack: out")
+        self._check(self.lib.skim_group_unpack(self.h, codes, scales, n, m, group, Wq.data_ptr()))
+        return Wq
+
+    def group_matmul(self, gq, x, x_scales=None, out=None, out_dtype=None):
+        """y = x W^T.  x: bfloat16 [T, m] or [m], or e4m3 with x_scales float32[T].  y: bfloat16 (or out_dtype float32) [T, n] or [n]."""
+        codes, scales, n, m, group = self._group_pointers(gq)
+        xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_matmul: x")
+        dtype, yt = self._result_type(out, out_dtype)
+        y = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_matmul: out")
+        self._check(self.lib.skim_group_matmul(self.h, codes, scales, n, m, group, xp, xt, ldx, xs, T, y.data_ptr(), yt))
+        return y
+
+    def group_matmul_dx(self, gq, dy, out=None, out_dtype=None):
+        """dx = dy W, the gradient of group_matmul to x.  dy: bfloat16 [T, n] or [n]; dx: bfloat16 (or out_dtype float32) [T, m] or [m]."""
+        codes, scales, n, m, group = self._group_pointers(gq)
+        dyp, ld, T = self._rows(dy, (self.torch.bfloat16,), n, "group_matmul_dx: dy")
+        dtype, yt = self._result_type(out, out_dtype)
+        dx = self._result(out, (m,) if dy.dim() == 1 else (T, m), dtype, "group_matmul_dx: out")
+        self._check(self.lib.skim_group_matmul_dx(self.h, codes, scales, n, m, group, dyp, ld, T, dx.data_ptr(), yt))
+        return dx
+
+    def group_glu(self, gate, up, x, x_scales=None, out=None, out_dtype=None):
+        """silu(x Wg^T) * (x Wu^T) with two matrices of one shape and group; x and the result as in group_matmul."""
+        gc, gs, n, m, group = self._group_pointers(gate)
+        uc, us, *shape = self._group_pointers(up)
+        assert shape == [n, m, group], "group_glu: gate and up must agree in n, m and group"
+        xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_glu: x")
+        dtype, yt = self._result_type(out, out_dtype)
+        a = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_glu: out")
+        self._check(self.lib.skim_group_glu(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, a.data_ptr(), yt))
+        return a
+
+    def group_glu_backward(self, gate, up, x, da, x_scales=None, want_dx=True, out=None):
+        """Gradients of group_glu for da (bfloat16, shape of its result): dict(dx [T, m], dgate, dup [T, n]), bfloat16.  g and u are
+        worked out again from x."""
+        t = self.torch
+        gc, gs, n, m, group = self._group_pointers(gate)
+        uc, us, *shape = self._group_pointers(up)
+        assert shape == [n, m, group], "group_glu_backward: gate and up must agree in n, m and group"
+        xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_glu_backward: x")
+        dap, ldda, rows = self._rows(da, (t.bfloat16,), n, "group_glu_backward: da")
+        assert rows == T and da.dim() == x.dim(), "group_glu_backward: da"
+        lead = () if x.dim() == 1 else (T,)
+        out = out or {}
+        dgate = self._result(out.get("dgate"), lead + (n,), t.bfloat16, "group_glu_backward: dgate")
+        dup = self._result(out.get("dup"), lead + (n,), t.bfloat16, "group_glu_backward: dup")
+        dx = self._result(out.get("dx"), lead + (m,), t.bfloat16, "group_glu_backward: dx") if want_dx else None
+        self._check(self.lib.skim_group_glu_backward(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, dap, ldda, dgate.data_ptr(),
+                                                     dup.data_ptr(), None if dx is None else dx.data_ptr(), BF16))
+        return dict(dx=dx, dgate=dgate, dup=dup)
+
+    # -- norm -----------------------------------------------------------------
+    def rms_norm(self, x, weight=None, residual=None, eps=1e-6, want_q=True, want_y=False, out=None):
+        """Root-mean-square norm of the rows of x (+ residual): bfloat16 or float32 [rows, m] or [m]; weight float32[m].  Returns
+        dict(h: x + residual, None without a residual; q, scales: e4m3 output and a scale a row; y: output in x's type; rstd float32[rows])."""
+        t = self.torch
+        m = x.shape[-1]
+        xp, ldx, rows = self._rows(x, (t.bfloat16, t.float32), m, "rms_norm: x")
+        rp, ldr = None, 0
+        if residual is not None:
+            assert residual.dtype == x.dtype and residual.shape == x.shape, "rms_norm: residual"
+            rp, ldr, _ = self._rows(residual, (x.dtype,), m, "rms_norm: residual")
+        wp = self._norm_weight(weight, m)
+        out = out or {}
+        h = self._result(out.get("h"), x.shape, x.dtype, "rms_norm: h") if residual is not None else None
+        y = self._result(out.get("y"), x.shape, x.dtype, "rms_norm: y") if want_y else None
+        q = self._result(out.get("q"), x.shape, t.float8_e4m3fn, "rms_norm: q") if want_q else None
+        scales = self._result(out.get("scales"), (rows,), t.float32, "rms_norm: scales") if want_q else None
+        rstd = self._result(out.get("rstd"), (rows,), t.float32, "rms_norm: rstd")
+        self._check(self.lib.skim_rms_norm(self.h, xp, ldx, rp, ldr, BF16 if x.dtype == t.bfloat16 else F32, wp, eps, rows, m,
+                                           None if h is None else h.data_ptr(), None if y is None else y.data_ptr(),
+                                           None if q is None else q.data_ptr(), None if scales is None else scales.data_ptr(), rstd.data_ptr()))
+        return dict(h=h, q=q, scales=scales, y=y, rstd=rstd)
+
+    def _norm_weight(self, weight, m):
+        if weight is None:
+            return None
+        assert weight.dtype == self.torch.float32 and weight.shape == (m,) and weight.is_contiguous() and weight.device == self.device, "weight"
+        return weight.data_ptr()
+
+    def rms_norm_backward(self, dy, h, rstd, weight=None, dh=None, want_dweight=True, out=None):
+        """Gradients of rms_norm: dy to its output, h and rstd as it returned them (h: x where there was no residual), dh to h past the
+        norm.  Returns dict(dx in dy's type: to x and to the residual; dweight float32[m])."""
+        t = self.torch
+        m = dy.shape[-1]
+        dyp, lddy, rows = self._rows(dy, (t.bfloat16, t.float32), m, "rms_norm_backward: dy")
+        assert h.dtype == dy.dtype and h.shape == dy.shape, "rms_norm_backward: h"
+        hp, ldh, _ = self._rows(h, (dy.dtype,), m, "rms_norm_backward: h")
+        dhp, lddh = None, 0
+        if dh is not None:
+            assert dh.dtype == dy.dtype and dh.shape == dy.shape, "rms_norm_backward: dh"
+            dhp, lddh, _ = self._rows(dh, (dy.dtype,), m, "rms_norm_backward: dh")
+        assert rstd.dtype == t.float32 and rstd.numel() == rows and rstd.is_contiguous() and rstd.device == self.device, "rms_norm_backward: rstd"
+        wp = self._norm_weight(weight, m)
+        out = out or {}
+        dx = self._result(out.get("dx"), dy.shape, dy.dtype, "rms_norm_backward: dx")
+        dweight, scratch, need = None, None, 0
+        if want_dweight:
+            dweight = self._result(out.get("dweight"), (m,), t.float32, "rms_norm_backward: dweight")
+            need = int(self.lib.skim_rms_norm_scratch_bytes(self.h, rows, m))
+            scratch = self.empty((need,), t.uint8)       # (goes back to the allocator with the work on this stream queued ahead of its next use)
+        self._check(self.lib.skim_rms_norm_backward(self.h, dyp, lddy, hp, ldh, dhp, lddh, BF16 if dy.dtype == t.bfloat16 else F32,
+                                                    rstd.data_ptr(), wp, rows, m, dx.data_ptr(), None if dweight is None else dweight.data_ptr(),
+                                                    None if scratch is None else scratch.data_ptr(), need))
+        return dict(dx=dx, dweight=dweight)
 
     def train_scale(self, W, S, H, bits, alpha, adam_m, adam_v, steps=120, outer=1, t0=1, kmeans_iters=30, opts=None):
         """Alg. 2 as one call; alpha, adam_m, adam_v are updated in place.  Returns labels, centroids, loss_trace."""
