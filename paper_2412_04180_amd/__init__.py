@@ -162,8 +162,9 @@ class Context:
         self.device = torch.device("cuda", device)
         torch.cuda.set_device(self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._raw_stream = self.stream.cuda_stream
         h = C.c_void_p()
-        st = self.lib.skim_create(C.byref(h), device, C.c_void_p(self.stream.cuda_stream))
+        st = self.lib.skim_create(C.byref(h), device, C.c_void_p(self._raw_stream))
         if st != SKIM_OK:
             raise SkimError(st, self.lib.skim_last_error(None).decode())
         self.h = h
@@ -212,8 +213,12 @@ class Context:
         return a.value, b.value
 
     def empty(self, shape, dtype):
-        with self.torch.cuda.stream(self.stream):     # outputs belong to the stream the kernels run on
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
+        t = self.torch
+        # outputs belong to the stream the kernels run on; entering it takes longer than a short kernel, and is left out where it is current
+        if t._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
+            return t.empty(shape, dtype=dtype, device=self.device)
+        with t.cuda.stream(self.stream):
+            return t.empty(shape, dtype=dtype, device=self.device)
 
     # -- clustering -----------------------------------------------------------
     def error_table(self, W, S, alpha=None, bmin=1, bmax=4, iters=30, want_centroids=True, want_upper=True,

@@ -3,7 +3,9 @@
 // All of them run on the matrix cores with exact operands: a code is a whole number, a code times its scale a bfloat16, and x comes in
 // bfloat16 or e4m3.  Sums are float32; the one rounding is that of a result to its type.
 #include "skim_group.h"
+#include "skim_tiles.h"
 
+#include <initializer_list>
 #include <type_traits>
 
 namespace {
@@ -27,6 +29,7 @@ struct MmArgs {
     const uint16_t *da;          // backward pass of the gated block
     long long ldda;
     uint16_t *dgate, *dup;
+    bool quads;                  // results (and da) can be taken in fours
 };
 
 enum { MM_PLAIN, MM_GLU, MM_GLU_BACK };
@@ -35,18 +38,56 @@ __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast
 __device__ __forceinline__ float from_bf16(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 __device__ __forceinline__ float sigmoid(float g) { return 1.f / (1.f + expf(-g)); }
 
-// One result: row and token are inside.
+// Four neighbouring results of a token, of rows `row` .. row + 3 of `rows`; the token is inside.  Sums come times `by`.
 template <int MODE>
-__device__ __forceinline__ void finish(const MmArgs &A, long long t, long long row, float g, float u) {
-    if (MODE == MM_GLU_BACK) {
-        const float d = from_bf16(A.da[t * A.ldda + row]), s = sigmoid(g);
-        A.dgate[t * A.n + row] = to_bf16(d * u * s * fmaf(g, 1.f - s, 1.f));
-        A.dup[t * A.n + row] = to_bf16(d * g * s);
+__device__ __forceinline__ void finish4(const MmArgs &A, long long t, long long row, long long rows, gq_float4 g, gq_float4 u, float by) {
+    if (row >= rows) return;
+    const long long at = t * rows + row;
+    const bool quad = A.quads;                    // rows come in fours, everything on borders of fours
+    if constexpr (MODE == MM_GLU_BACK) {
+        gq_short4 d = {}, dg, du;
+        const uint16_t *p = A.da + t * A.ldda + row;
+        if (quad) d = *(const gq_short4 *)p;
+        else
+            for (int i = 0; i < 4; ++i)
+                if (row + i < rows) d[i] = (short)p[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float gi = g[i] * by, ui = u[i] * by, di = from_bf16((uint16_t)d[i]), s = sigmoid(gi);
+            dg[i] = (short)to_bf16(di * ui * s * fmaf(gi, 1.f - s, 1.f));
+            du[i] = (short)to_bf16(di * gi * s);
+        }
+        if (quad) {
+            *(gq_short4 *)(A.dgate + at) = dg;
+            *(gq_short4 *)(A.dup + at) = du;
+        } else {
+            for (int i = 0; i < 4; ++i)
+                if (row + i < rows) A.dgate[at + i] = (uint16_t)dg[i], A.dup[at + i] = (uint16_t)du[i];
+        }
         return;
     }
-    const float v = MODE == MM_GLU ? g * sigmoid(g) * u : g;
-    if (A.y_f32) ((float *)A.y)[t * A.n + row] = v;
-    else ((uint16_t *)A.y)[t * A.n + row] = to_bf16(v);
+    gq_float4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float gi = g[i] * by;
+        v[i] = MODE == MM_GLU ? gi * sigmoid(gi) * (u[i] * by) : gi;
+    }
+    if (A.y_f32) {
+        float *p = (float *)A.y + at;
+        if (quad) *(gq_float4 *)p = v;
+        else
+            for (int i = 0; i < 4; ++i)
+                if (row + i < rows) p[i] = v[i];
+    } else {
+        uint16_t *p = (uint16_t *)A.y + at;
+        gq_short4 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = (short)to_bf16(v[i]);
+        if (quad) *(gq_short4 *)p = o;
+        else
+            for (int i = 0; i < 4; ++i)
+                if (row + i < rows) p[i] = (uint16_t)o[i];
+    }
 }
 
 // ---- operands ------------------------------------------------------------------------------------------------------------
@@ -84,10 +125,14 @@ __device__ __forceinline__ gq_bf16x8 load_x(const void *x, long long row0, long 
     if constexpr (VEC) {
         if (col < m) v = *(const V *)p;
     } else {
-        E e[8];
+        if (col + 8 <= m) {
+            __builtin_memcpy(&v, p, sizeof(v));              // (one load, of any alignment)
+        } else {
+            E e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = col + i < m ? p[i] : (E)0;
-        __builtin_memcpy(&v, e, sizeof(v));
+            for (int i = 0; i < 8; ++i) e[i] = col + i < m ? p[i] : (E)0;
+            __builtin_memcpy(&v, e, sizeof(v));
+        }
     }
     if constexpr (XT == SKIM_BF16) return __builtin_bit_cast(gq_bf16x8, v);
     else return widen(v);
@@ -100,7 +145,7 @@ __device__ __forceinline__ gq_bf16x8 load_x(const void *x, long long row0, long 
 template <int XT, int NT, int G, int MODE, bool VEC>
 __global__ void __launch_bounds__(1024) group_few_kernel(MmArgs A, int chunks) {
     constexpr int MATS = MODE == MM_PLAIN ? 1 : 2;
-    extern __shared__ float red[];
+    extern __shared__ __align__(16) unsigned char few_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nw = blockDim.x >> 6;
     const int c = lane >> 4, l16 = lane & 15;
     const long long rt = blockIdx.x / chunks, t0 = (long long)(blockIdx.x % chunks) * (16 * NT);
@@ -139,90 +184,232 @@ __global__ void __launch_bounds__(1024) group_few_kernel(MmArgs A, int chunks) {
             }
         }
     }
-    constexpr int E = NT * 4 * 64;       // sums of a wavefront, for one matrix
+    constexpr int E = NT * 64;           // fours of a wavefront's sums, for one matrix
+    gq_float4 *red = (gq_float4 *)few_lds;
 #pragma unroll
     for (int a = 0; a < MATS; ++a)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) red[((wave * MATS + a) * NT + j) * 256 + i * 64 + lane] = acc[a][j][i];
+        for (int j = 0; j < NT; ++j) red[((wave * MATS + a) * NT + j) * 64 + lane] = acc[a][j];
     __syncthreads();
     for (int e = tid; e < E; e += blockDim.x) {
-        float v[MATS];
+        gq_float4 v[MATS] = {};
 #pragma unroll
-        for (int a = 0; a < MATS; ++a) {
-            v[a] = 0.f;
+        for (int a = 0; a < MATS; ++a)
             for (int w = 0; w < nw; ++w) v[a] += red[(w * MATS + a) * E + e];
-        }
         const int el = e & 63;
-        const long long t = t0 + 16 * (e >> 8) + (el & 15), row = rt * GQ_ROWS + 4 * (el >> 4) + ((e >> 6) & 3);
-        if (t < A.T && row < A.n) {
-            const float by = XT == SKIM_E4M3 ? A.x_scales[t] : 1.f;
-            finish<MODE>(A, t, row, v[0] * by, MATS == 2 ? v[MATS - 1] * by : 0.f);
-        }
+        const long long t = t0 + 16 * (e >> 6) + (el & 15);
+        if (t < A.T) finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
     }
 }
 
-// ---- gradient to the input -------------------------------------------------------------------------------------------------
+// ---- many tokens -----------------------------------------------------------------------------------------------------------
 
-// dx = dy W (+ dy2 W2): a workgroup makes 128 columns for 64 tokens, a wavefront 32 of them.  32 rows a step: the codes of two row blocks
-// become scaled bfloat16 values in LDS, and the transposing reads give each lane 8 rows of its column.
-template <int G, bool VEC>
-__global__ void __launch_bounds__(256) group_dx_kernel(MmArgs A, int mats, int chunks) {
-    __shared__ __align__(16) uint16_t tile[4][32][32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane >> 4, l16 = lane & 15;
-    const long long kb = blockIdx.x / chunks, t0 = (long long)(blockIdx.x % chunks) * 64;
+// y = x W^T, the gated block and its backward pass, and dx = dy W (+ dy2 W2), on tiles of the matrix cores.  A workgroup of four wavefronts makes
+// 256 rows of W (128 of gate and the same of up; for dx 256 columns) for 128 tokens, a wavefront 64 of them: 4 x 8 accumulator
+// tiles of 16 x 16.
+// The tokens' operand: 128 columns of x (rows of dy's matrix for dx) go to LDS a block ahead, in bfloat16.  The weights' operand never is in
+// memory: codes come into registers a block ahead, one 16-byte load for 32 of them, and are taken apart there, times their scale, into
+// operands.  For dx, where a lane needs 8 rows of one column, they pass through 4 KB of LDS of the wavefront's own and come back by the transposing read.
+// LDS rows of a token are 256 bytes; its 16-byte unit u is at place u ^ (token % 16), so that 16 tokens' units of one column octet lie in different banks.
+constexpr int WIDE_TOKENS = 128, WIDE_THREADS = 256, WIDE_TT = WIDE_TOKENS / 16, WIDE_RT = 4;
+constexpr int WIDE_X_BYTES = WIDE_TOKENS * GQ_COLS * 2;              // of one block: 32 KB
+constexpr int WIDE_A_BYTES = 32 * 64 * 2;                            // dx: a wavefront's 32 rows x 64 columns
+constexpr int WIDE_UNITS = WIDE_X_BYTES / 16 / WIDE_THREADS;         // 16-byte units of a thread: 8
+
+// Scaled weights of a word, exact in bfloat16.
+__device__ __forceinline__ gq_word4 weight_operand(uint32_t w, float s) {
+    gq_word4 v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t bytes = h ? gq_high(w) : gq_low(w);
+        const gq_float2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, true);
+        v[2 * h] = __builtin_amdgcn_perm(__float_as_uint(s * a.y), __float_as_uint(s * a.x), 0x07060302u);
+        v[2 * h + 1] = __builtin_amdgcn_perm(__float_as_uint(s * b.y), __float_as_uint(s * b.x), 0x07060302u);
+    }
+    return v;
+}
+
+enum { STAGE_COPY, STAGE_BF16, STAGE_E4M3 };       // straight into LDS; through registers: bfloat16 of any alignment, e4m3
+
+template <bool DX, int MODE, int STAGE>
+__global__ void __launch_bounds__(WIDE_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) group_wide_kernel(MmArgs A, int group, int mats, int ttiles) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane >> 4, l16 = lane & 15;
+    const int tile = xcd_order(blockIdx.x, gridDim.x);
+    const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * WIDE_TOKENS;
     const long long kbs = gq_col_blocks(A.m), rbs = gq_row_blocks(A.n), n16 = rbs * GQ_ROWS;
-    long long xrow[4];
+    const long long depth = DX ? A.n : A.m;                          // summed over
+    const int blocks = (int)((depth + 127) / 128), total = DX ? blocks * mats : blocks;
+    const int per = GQ_COLS / group;
+
+    // ---- the tokens' operand
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte *)smem;
+    const int es = STAGE == STAGE_E4M3 ? 1 : 2;
+    uint32_t voff[WIDE_UNITS];
+    gq_word2 held[WIDE_UNITS];                                       // e4m3: the next block's units on their way
 #pragma unroll
-    for (int j = 0; j < 4; ++j) xrow[j] = min(t0 + 16 * j + l16, A.T - 1) * A.ldx;
-    gq_float4 acc[2][4] = {};
-    for (int a = 0; a < mats; ++a) {
-        for (long long rb = 0; rb < rbs; rb += 2) {
+    for (int i = 0; i < WIDE_UNITS; ++i) {
+        const int t = (wave * WIDE_UNITS + i) * 4 + c;               // (copies: 4 tokens of 16 units each)
+        voff[i] = (uint32_t)(min((long long)t, A.T - 1 - t0) * A.ldx * es) + (uint32_t)((l16 ^ (t & 15)) * 8 * es);
+    }
+    auto xbase = [&](int kb) -> const unsigned char * {
+        const int a = DX ? kb / blocks : 0;
+        return (const unsigned char *)(a ? A.x2 : A.x) + (t0 * A.ldx + (long long)(kb - a * blocks) * GQ_COLS) * es;
+    };
+    auto columns_left = [&](int kb) -> int { return (int)min(depth - (long long)(kb % blocks) * GQ_COLS, 128ll); };
+    auto unit_column = [&](int i) -> int { return (l16 ^ ((i * 4 + c) & 15)) * 8; };
+    auto stage = [&](int kb) {
+        const int left = columns_left(kb);
+        const uint32_t dst = lds0 + (uint32_t)(kb & 1) * WIDE_X_BYTES + (uint32_t)wave * (WIDE_X_BYTES / 4);
+        if constexpr (STAGE == STAGE_COPY) {
+            const LdsSource src{(uint64_t)(uintptr_t)xbase(kb), 0x7FFFFFFF};
+            const int4v rs = src.rsrc();
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                gq_word4 v = {};
-                if (rb + h < rbs) {
-                    const uint32_t w = A.codes[a][((rb + h) * kbs + kb) * 64 + lane][wave];
-                    const float s = gq_scale(A.scales[a][(kb * (GQ_COLS / G) + 32 * wave / G) * n16 + (rb + h) * GQ_ROWS + l16]);
+            for (int i = 0; i < WIDE_UNITS; ++i) copy_to_lds(dst + i * 1024, unit_column(i) < left ? voff[i] : 0x80000000u, rs);
+        } else if constexpr (STAGE == STAGE_E4M3) {
+            const unsigned char *x = xbase(kb);
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const uint32_t bytes = p < 2 ? gq_low(w) : gq_high(w);
-                        const gq_float2 f = p & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, true)
-                                                  : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, false);
-                        v[p] = __builtin_amdgcn_perm(__float_as_uint(s * f.y), __float_as_uint(s * f.x), 0x07060302u);
-                    }
+            for (int i = 0; i < WIDE_UNITS; ++i) {
+                held[i] = gq_word2{};
+                const int over = unit_column(i) - left;
+                if (over <= -8) __builtin_memcpy(&held[i], x + voff[i], 8);
+                else if (over < 0) {
+                    uint8_t e[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) e[q] = over + q < 0 ? x[voff[i] + q] : (uint8_t)0;
+                    __builtin_memcpy(&held[i], e, 8);
                 }
-                *(gq_word4 *)&tile[wave][16 * h + l16][8 * c] = v;
             }
-            __syncthreads();
-            gq_bf16x8 b[4];
-            const void *x = a ? A.x2 : A.x;
+        } else {
+            const unsigned char *x = xbase(kb);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = load_x<SKIM_BF16, VEC>(x, xrow[j], rb * GQ_ROWS + 8 * c, A.n);
+            for (int i = 0; i < WIDE_UNITS; ++i) {
+                gq_word4 v = {};
+                const int over = unit_column(i) - left;
+                if (over <= -8) __builtin_memcpy(&v, x + voff[i], 16);
+                else if (over < 0) {
+                    uint16_t e[8];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const gq_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)&tile[wave][8 * c + (l16 >> 2)][16 * p + 4 * (l16 & 3)]);
-                const gq_short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)&tile[wave][8 * c + 4 + (l16 >> 2)][16 * p + 4 * (l16 & 3)]);
-                const gq_bf16x8 q = __builtin_bit_cast(gq_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[p][j] = mfma(q, b[j], acc[p][j]);
+                    for (int q = 0; q < 8; ++q) e[q] = over + q < 0 ? ((const uint16_t *)(x + voff[i]))[q] : (uint16_t)0;
+                    __builtin_memcpy(&v, e, 16);
+                }
+                *(gq_word4 *)(smem + (dst - lds0) + i * 1024 + lane * 16) = v;
             }
-            __syncthreads();
+        }
+    };
+    auto store_held = [&](int kb) {
+        unsigned char *dst = smem + (kb & 1) * WIDE_X_BYTES + wave * (WIDE_X_BYTES / 4);
+#pragma unroll
+        for (int i = 0; i < WIDE_UNITS; ++i) *(gq_bf16x8 *)(dst + i * 1024 + lane * 16) = widen(held[i]);
+    };
+
+    // ---- the weights' operand
+    constexpr int PAIR = MODE == MM_PLAIN ? 4 : 2;                   // row blocks of a wavefront, of one matrix
+    const long long rb0 = (ob * 4 + wave) * PAIR;
+    const long long cb = min(ob * 2 + (wave >> 1), kbs - 1);         // dx: column block, and which half of it
+    const int half = wave & 1;
+    gq_word4 next[4];
+    uint32_t nscale[4];
+    auto load_codes = [&](int kb) {
+        if constexpr (DX) {
+            const int a = kb / blocks;
+            const long long rb = (long long)(kb - a * blocks) * 8;
+            const uint32_t *w = (const uint32_t *)A.codes[a] + (cb * 64 + lane) * 4 + 2 * half;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                gq_word2 v = {};
+                if (rb + j < rbs) v = *(const gq_word2 *)(w + (rb + j) * kbs * 256);
+                next[j >> 1][2 * (j & 1)] = v[0];
+                next[j >> 1][2 * (j & 1) + 1] = v[1];
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)                              // word q / 2 of the half, rows q % 2 * 64 + lane
+                nscale[q] = A.scales[a][(cb * per + (64 * half + 32 * (q >> 1)) / group) * n16 + min(rb * GQ_ROWS + 64 * (q & 1) + lane, n16 - 1)];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) next[i] = A.codes[i / PAIR][(min(rb0 + i % PAIR, rbs - 1) * kbs + kb) * 64 + lane];
+            const uint16_t *s = A.scales[c / PAIR] + min(rb0 + c % PAIR, rbs - 1) * GQ_ROWS + l16;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) nscale[q] = s[((long long)kb * per + 32 * q / group) * n16];
+        }
+    };
+    gq_word4 cur[4];
+    uint32_t cscale[4];
+    unsigned char *mine = smem + 2 * WIDE_X_BYTES + wave * WIDE_A_BYTES;
+    auto flip = [](int row) { return (2 * (row & 3)) ^ ((row >> 2) & 1); };    // dx: unit u of a row is at u ^ flip(row)
+    auto operands = [&](int k, gq_bf16x8 (&a)[4]) {
+        if constexpr (DX) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {                            // row block p / 2 of the step, word p % 2
+                const int j = 2 * k + (p >> 1), q = p & 1;
+                const float s = gq_scale((uint32_t)__shfl((int)cscale[2 * q + (j >> 2)], 16 * (j & 3) + l16, 64));
+                const int row = 16 * (p >> 1) + l16;
+                *(gq_word4 *)(mine + row * 128 + ((4 * q + c) ^ flip(row)) * 16) = weight_operand(cur[j >> 1][2 * (j & 1) + q], s);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 8 * c + (l16 >> 2), u = 2 * i + ((l16 & 3) >> 1);
+                const gq_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(mine + row * 128 + (u ^ flip(row)) * 16 + (l16 & 1) * 8));
+                const gq_short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(mine + (row + 4) * 128 + (u ^ flip(row + 4)) * 16 + (l16 & 1) * 8));
+                a[i] = __builtin_bit_cast(gq_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float s = gq_scale((uint32_t)__shfl((int)cscale[k], 16 * i + l16, 64));
+                a[i] = __builtin_bit_cast(gq_bf16x8, weight_operand(cur[i][k], s));
+            }
+        }
+    };
+
+    gq_float4 acc[WIDE_RT][WIDE_TT] = {};
+    stage(0);
+    load_codes(0);
+    if constexpr (STAGE == STAGE_E4M3) store_held(0);
+    for (int kb = 0; kb < total; ++kb) {
+        // this block's copies have landed, its codes too, and everybody is done with the block before, whose place the next one takes
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            cur[i] = next[i];
+            cscale[i] = nscale[i];
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier"
+                     : "+v"(cur[0]), "+v"(cur[1]), "+v"(cur[2]), "+v"(cur[3]), "+v"(cscale[0]), "+v"(cscale[1]), "+v"(cscale[2]), "+v"(cscale[3])
+                     :
+                     : "memory");
+        if (kb + 1 < total) {
+            stage(kb + 1);
+            load_codes(kb + 1);
+        }
+        const unsigned char *xb = smem + (kb & 1) * WIDE_X_BYTES + l16 * 256;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            gq_bf16x8 a[4];
+            operands(k, a);
+#pragma unroll
+            for (int j = 0; j < WIDE_TT; ++j) {
+                const gq_bf16x8 b = *(const gq_bf16x8 *)(xb + j * 4096 + (((4 * k + c) ^ l16) << 4));
+#pragma unroll
+                for (int i = 0; i < WIDE_RT; ++i) acc[i][j] = mfma(a[i], b, acc[i][j]);
+            }
+        }
+        if constexpr (STAGE == STAGE_E4M3) {
+            if (kb + 1 < total) store_held(kb + 1);
         }
     }
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+    for (int j = 0; j < WIDE_TT; ++j) {
+        const long long t = t0 + 16 * j + l16;
+        if (t >= A.T) continue;
+        const float by = STAGE == STAGE_E4M3 ? A.x_scales[t] : 1.f;
+        if constexpr (DX) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int i = 0; i < 4; ++i) finish4<MM_PLAIN>(A, t, (ob * 4 + wave) * 64 + 16 * i + 4 * c, A.m, acc[i][j], acc[i][j], 1.f);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const long long t = t0 + 16 * j + l16, col = kb * GQ_COLS + 32 * wave + 16 * p + 4 * c + i;
-                if (t < A.T && col < A.m) {
-                    if (A.y_f32) ((float *)A.y)[t * A.m + col] = acc[p][j][i];
-                    else ((uint16_t *)A.y)[t * A.m + col] = to_bf16(acc[p][j][i]);
-                }
-            }
+            for (int i = 0; i < PAIR; ++i) finish4<MODE>(A, t, (rb0 + i) * GQ_ROWS + 4 * c, A.n, acc[i][j], acc[MODE == MM_PLAIN ? i : i + PAIR][j], by);
+        }
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -234,9 +421,45 @@ void with_group(int group, F &&f) {
     else f(std::integral_constant<int, 128>{});
 }
 
+// From so many tokens on the tiles of 128 pay.
+constexpr int64_t WIDE_FROM = 65;
+
+bool all_on(int64_t border, std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if ((uintptr_t)p % border) return false;
+    return true;
+}
+
+template <bool DX, int MODE>
+skim_status launch_wide(skim_ctx *ctx, const MmArgs &A, int group, int x_type, int mats) {
+    const int64_t out = DX ? A.m : A.n, per = MODE == MM_PLAIN ? 256 : 128;
+    const int64_t ttiles = (A.T + WIDE_TOKENS - 1) / WIDE_TOKENS, tiles = (out + per - 1) / per * ttiles, depth = DX ? A.n : A.m;
+    if (tiles > 0x7fffffff || A.ldx >= (1 << 23) || depth > (1 << 24))
+        SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens of row stride %lld are too many for one call", A.T, A.ldx);
+    const size_t lds = 2 * WIDE_X_BYTES + (DX ? 4 * WIDE_A_BYTES : 0);
+    const bool copy = x_type == SKIM_BF16 && depth % 8 == 0 && A.ldx % 8 == 0 && all_on(16, {A.x, A.x2});
+    auto go = [&](auto stage) -> hipError_t {
+        auto *k = &group_wide_kernel<DX, MODE, decltype(stage)::value>;
+        hipError_t e = hipSuccess;
+        if (lds > 64 * 1024) e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e == hipSuccess) hipLaunchKernelGGL(k, dim3((unsigned)tiles), dim3(WIDE_THREADS), lds, ctx->stream, A, group, mats, (int)ttiles);
+        return e;
+    };
+    hipError_t e;
+    if (copy) e = go(std::integral_constant<int, STAGE_COPY>{});
+    else if (x_type == SKIM_BF16) e = go(std::integral_constant<int, STAGE_BF16>{});
+    else if constexpr (!DX) e = go(std::integral_constant<int, STAGE_E4M3>{});
+    else SKIM_FAIL(ctx, SKIM_ERR_ARG, "gradients are bfloat16");
+    SKIM_HIP(ctx, e);
+    SKIM_HIP(ctx, hipGetLastError());
+    return SKIM_OK;
+}
+
 template <int MODE>
-skim_status launch_forward(skim_ctx *ctx, const MmArgs &A, int group, int x_type) {
+skim_status launch_forward(skim_ctx *ctx, MmArgs A, int group, int x_type) {
+    A.quads = A.n % 4 == 0 && all_on(16, {A.y, A.dgate, A.dup}) && (!A.da || (A.ldda % 4 == 0 && all_on(8, {A.da})));
     constexpr int MATS = MODE == MM_PLAIN ? 1 : 2;
+    if (A.T >= WIDE_FROM) return launch_wide<false, MODE>(ctx, A, group, x_type, 1);
     const int nt = A.T <= 16 ? 1 : A.T <= 32 ? 2 : 4;
     const int64_t chunks = (A.T + 16 * nt - 1) / (16 * nt), groups = gq_row_blocks(A.n) * chunks;
     if (groups > 0x7fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens on %lld rows are too many for one call", A.T, A.n);
@@ -266,19 +489,9 @@ skim_status launch_forward(skim_ctx *ctx, const MmArgs &A, int group, int x_type
     return SKIM_OK;
 }
 
-skim_status launch_dx(skim_ctx *ctx, const MmArgs &A, int group, int mats) {
-    const int64_t chunks = (A.T + 63) / 64, groups = gq_col_blocks(A.m) * chunks;
-    if (groups > 0x7fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens on %lld columns are too many for one call", A.T, A.m);
-    const bool vec = A.n % 8 == 0 && A.ldx % 8 == 0 && (((uintptr_t)A.x | (uintptr_t)A.x2) & 15) == 0;
-    with_group(group, [&](auto g) {
-        auto go = [&](auto v) {
-            hipLaunchKernelGGL((group_dx_kernel<decltype(g)::value, decltype(v)::value>), dim3((unsigned)groups), dim3(256), 0, ctx->stream, A, mats, (int)chunks);
-        };
-        if (vec) go(std::true_type{});
-        else go(std::false_type{});
-    });
-    SKIM_HIP(ctx, hipGetLastError());
-    return SKIM_OK;
+skim_status launch_dx(skim_ctx *ctx, MmArgs A, int group, int mats) {
+    A.quads = A.m % 4 == 0 && all_on(16, {A.y});
+    return launch_wide<true, MM_PLAIN>(ctx, A, group, SKIM_BF16, mats);
 }
 
 skim_status check_x(skim_ctx *ctx, const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, int64_t m, const char *who) {
