@@ -316,11 +316,17 @@ skim_status skim_group_unpack(skim_ctx *ctx, const uint32_t *codes, const uint16
  * x: dev, SKIM_BF16 with x_scales NULL, or SKIM_E4M3 with x_scales dev float32[T]: token t is x_scales[t] times its row of x (what
  * skim_rms_norm writes).  Row strides ldx >= m, lddy >= n in elements; any alignment, but rows on 16-byte borders (8-byte ones for
  * e4m3) whose length is a multiple of 8 are read faster.  Results: SKIM_BF16 or SKIM_F32, dense, apart from all inputs.
- * Operands are exact and sums float32; a result is rounded once, to its type.  What x holds behind a row's m columns is not used. */
+ * Operands are exact and sums float32; a result is rounded once, to its type.  What x holds behind a row's m columns is not used.
+ * scratch (dev, 16-byte aligned; NULL with 0 bytes = none): where the results have few tiles, several compute units share one, and their sums
+ * meet there; skim_group_scratch_bytes(ctx, n, m, T) bytes (0 for most calls, at most 32 MB) are enough for any call of this section
+ * on these sizes, with fewer it is slower.  The order of the sums, and so their last digits, depend on it. */
+size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T);
 skim_status skim_group_matmul(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
-                              const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, void *y, int y_type);
+                              const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, void *y, int y_type,
+                              void *scratch, size_t scratch_bytes);
 skim_status skim_group_matmul_dx(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
-                                 const uint16_t *dy_bf16, int64_t lddy, int64_t T, void *dx, int dx_type);
+                                 const uint16_t *dy_bf16, int64_t lddy, int64_t T, void *dx, int dx_type,
+                                 void *scratch, size_t scratch_bytes);
 
 /* The gated half of a feed-forward block, both projections, the activation and the product in one pass:
  *   a = silu(x Wg^T) * (x Wu^T),   silu(g) = g / (1 + exp(-g))
@@ -332,11 +338,11 @@ skim_status skim_group_matmul_dx(skim_ctx *ctx, const uint32_t *codes, const uin
  * the token's row times its scale. */
 skim_status skim_group_glu(skim_ctx *ctx, const uint32_t *gate_codes, const uint16_t *gate_scales, const uint32_t *up_codes,
                            const uint16_t *up_scales, int64_t n, int64_t m, int group, const void *x, int x_type, int64_t ldx,
-                           const float *x_scales, int64_t T, void *a, int a_type);
+                           const float *x_scales, int64_t T, void *a, int a_type, void *scratch, size_t scratch_bytes);
 skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *gate_codes, const uint16_t *gate_scales, const uint32_t *up_codes,
                                     const uint16_t *up_scales, int64_t n, int64_t m, int group, const void *x, int x_type, int64_t ldx,
                                     const float *x_scales, int64_t T, const uint16_t *da_bf16, int64_t ldda, uint16_t *dgate_bf16,
-                                    uint16_t *dup_bf16, void *dx, int dx_type);
+                                    uint16_t *dup_bf16, void *dx, int dx_type, void *scratch, size_t scratch_bytes);
 
 /* Root-mean-square norm, with the residual's addition ahead of it and an 8-bit output for the products above:
  *   h = x + residual (rounded to the type; without a residual h is x),  rstd = 1 / sqrt(mean_j h_j^2 + eps),  y_j = h_j rstd weight_j

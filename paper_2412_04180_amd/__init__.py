@@ -27,7 +27,7 @@ EXPORTS = ["skim_create", "skim_destroy", "skim_last_error", "skim_workspace_byt
            "skim_profile_enable", "skim_profile_last", "skim_validate_enable",
            "skim_error_table", "skim_error_table_lfull", "skim_cluster_rows", "skim_select_allocated", "skim_greedy_allocate", "skim_greedy_allocate_device",
            "skim_dp_allocate_scratch_bytes", "skim_dp_allocate", "skim_kmeans_optimal_scratch_bytes", "skim_kmeans_optimal",
-           "skim_packed_words", "skim_codebook_entries", "skim_pack", "skim_pack_static", "skim_layer_loss", "skim_scale_step", "skim_train_scale", "skim_unpack", "skim_dequant_matvec", "skim_dequant_matvec_f32", "skim_group_code_words", "skim_group_scale_entries", "skim_group_quantize", "skim_group_unpack", "skim_group_matmul", "skim_group_matmul_dx",
+           "skim_packed_words", "skim_codebook_entries", "skim_pack", "skim_pack_static", "skim_layer_loss", "skim_scale_step", "skim_train_scale", "skim_unpack", "skim_dequant_matvec", "skim_dequant_matvec_f32", "skim_group_code_words", "skim_group_scale_entries", "skim_group_quantize", "skim_group_unpack", "skim_group_scratch_bytes", "skim_group_matmul", "skim_group_matmul_dx",
            "skim_group_glu", "skim_group_glu_backward", "skim_rms_norm", "skim_rms_norm_scratch_bytes", "skim_rms_norm_backward",
            "skim_hessian_workspace_bytes", "skim_hessian_from_activations", "skim_hessian_from_activations_scratch"]
 
@@ -102,10 +102,12 @@ def load_library():
         lib.skim_group_scale_entries.restype = i64
         lib.skim_group_quantize.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp]
         lib.skim_group_unpack.argtypes = [vp, vp, vp, i64, i64, i32, vp]
-        lib.skim_group_matmul.argtypes = [vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32]
-        lib.skim_group_matmul_dx.argtypes = [vp, vp, vp, i64, i64, i32, vp, i64, i64, vp, i32]
-        lib.skim_group_glu.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32]
-        lib.skim_group_glu_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i64, vp, vp, vp, i32]
+        lib.skim_group_scratch_bytes.argtypes = [vp, i64, i64, i64]
+        lib.skim_group_scratch_bytes.restype = C.c_size_t
+        lib.skim_group_matmul.argtypes = [vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, vp, C.c_size_t]
+        lib.skim_group_matmul_dx.argtypes = [vp, vp, vp, i64, i64, i32, vp, i64, i64, vp, i32, vp, C.c_size_t]
+        lib.skim_group_glu.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, vp, C.c_size_t]
+        lib.skim_group_glu_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i64, vp, vp, vp, i32, vp, C.c_size_t]
         lib.skim_rms_norm.argtypes = [vp, vp, i64, vp, i64, i32, vp, C.c_float, i64, i64, vp, vp, vp, vp, vp]
         lib.skim_rms_norm_scratch_bytes.argtypes = [vp, i64, i64]
         lib.skim_rms_norm_scratch_bytes.restype = C.c_size_t
@@ -471,6 +473,14 @@ class Context:
         assert x_scales.numel() == T, what
         return p, E4M3, ld, x_scales.data_ptr(), T
 
+    def _group_scratch(self, n, m, T):
+        """(pointer, bytes, tensor) of the scratch of a product: it goes back to the allocator with this stream's work queued ahead of its next use."""
+        need = self.lib.skim_group_scratch_bytes(self.h, n, m, T)
+        if need == 0:
+            return None, 0, None
+        scratch = self.empty((need,), self.torch.uint8)
+        return scratch.data_ptr(), need, scratch
+
     def _result_type(self, out, out_dtype):
         dtype = out.dtype if out is not None else out_dtype if out_dtype is not None else self.torch.bfloat16
         assert dtype in (self.torch.bfloat16, self.torch.float32), "results are bfloat16 or float32"
@@ -504,7 +514,8 @@ class Context:
         xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_matmul: x")
         dtype, yt = self._result_type(out, out_dtype)
         y = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_matmul: out")
-        self._check(self.lib.skim_group_matmul(self.h, codes, scales, n, m, group, xp, xt, ldx, xs, T, y.data_ptr(), yt))
+        sp, sb, _keep = self._group_scratch(n, m, T)
+        self._check(self.lib.skim_group_matmul(self.h, codes, scales, n, m, group, xp, xt, ldx, xs, T, y.data_ptr(), yt, sp, sb))
         return y
 
     def group_matmul_dx(self, gq, dy, out=None, out_dtype=None):
@@ -513,7 +524,8 @@ class Context:
         dyp, ld, T = self._rows(dy, (self.torch.bfloat16,), n, "group_matmul_dx: dy")
         dtype, yt = self._result_type(out, out_dtype)
         dx = self._result(out, (m,) if dy.dim() == 1 else (T, m), dtype, "group_matmul_dx: out")
-        self._check(self.lib.skim_group_matmul_dx(self.h, codes, scales, n, m, group, dyp, ld, T, dx.data_ptr(), yt))
+        sp, sb, _keep = self._group_scratch(n, m, T)
+        self._check(self.lib.skim_group_matmul_dx(self.h, codes, scales, n, m, group, dyp, ld, T, dx.data_ptr(), yt, sp, sb))
         return dx
 
     def group_glu(self, gate, up, x, x_scales=None, out=None, out_dtype=None):
@@ -524,7 +536,8 @@ class Context:
         xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_glu: x")
         dtype, yt = self._result_type(out, out_dtype)
         a = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_glu: out")
-        self._check(self.lib.skim_group_glu(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, a.data_ptr(), yt))
+        sp, sb, _keep = self._group_scratch(n, m, T)
+        self._check(self.lib.skim_group_glu(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, a.data_ptr(), yt, sp, sb))
         return a
 
     def group_glu_backward(self, gate, up, x, da, x_scales=None, want_dx=True, out=None):
@@ -542,8 +555,9 @@ class Context:
         dgate = self._result(out.get("dgate"), lead + (n,), t.bfloat16, "group_glu_backward: dgate")
         dup = self._result(out.get("dup"), lead + (n,), t.bfloat16, "group_glu_backward: dup")
         dx = self._result(out.get("dx"), lead + (m,), t.bfloat16, "group_glu_backward: dx") if want_dx else None
+        sp, sb, _keep = self._group_scratch(n, m, T)
         self._check(self.lib.skim_group_glu_backward(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, dap, ldda, dgate.data_ptr(),
-                                                     dup.data_ptr(), None if dx is None else dx.data_ptr(), BF16))
+                                                     dup.data_ptr(), None if dx is None else dx.data_ptr(), BF16, sp, sb))
         return dict(dx=dx, dgate=dgate, dup=dup)
 
     # -- norm -----------------------------------------------------------------

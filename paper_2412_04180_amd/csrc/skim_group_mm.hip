@@ -5,6 +5,7 @@
 #include "skim_group.h"
 #include "skim_tiles.h"
 
+#include <algorithm>
 #include <initializer_list>
 #include <type_traits>
 
@@ -211,10 +212,9 @@ __global__ void __launch_bounds__(1024) group_few_kernel(MmArgs A, int chunks) {
 // memory: codes come into registers a block ahead, one 16-byte load for 32 of them, and are taken apart there, times their scale, into
 // operands.  For dx, where a lane needs 8 rows of one column, they pass through 4 KB of LDS of the wavefront's own and come back by the transposing read.
 // LDS rows of a token are 256 bytes; its 16-byte unit u is at place u ^ (token % 16), so that 16 tokens' units of one column octet lie in different banks.
-constexpr int WIDE_TOKENS = 128, WIDE_THREADS = 256, WIDE_TT = WIDE_TOKENS / 16, WIDE_RT = 4;
+constexpr int WIDE_TOKENS = 128, WIDE_R = 4, WIDE_THREADS = 64 * WIDE_R;
 constexpr int WIDE_X_BYTES = WIDE_TOKENS * GQ_COLS * 2;              // of one block: 32 KB
-constexpr int WIDE_A_BYTES = 32 * 64 * 2;                            // dx: a wavefront's 32 rows x 64 columns
-constexpr int WIDE_UNITS = WIDE_X_BYTES / 16 / WIDE_THREADS;         // 16-byte units of a thread: 8
+constexpr int WIDE_A_BYTES = 2 * 16 * 64 * 2;                        // dx: a wavefront's 16 rows x 64 columns, twice
 
 // Scaled weights of a word, exact in bfloat16.
 __device__ __forceinline__ gq_word4 weight_operand(uint32_t w, float s) {
@@ -229,187 +229,281 @@ __device__ __forceinline__ gq_word4 weight_operand(uint32_t w, float s) {
     return v;
 }
 
-enum { STAGE_COPY, STAGE_BF16, STAGE_E4M3 };       // straight into LDS; through registers: bfloat16 of any alignment, e4m3
+// Four sums of either row tile of wavefront `w` (counted through all tiles) for token t, those `in` rows down the tile.
+template <bool DX, int MODE>
+__device__ __forceinline__ void wide_finish(const MmArgs &A, long long w, long long t, int in, gq_float4 v0, gq_float4 v1) {
+    if (t >= A.T) return;
+    const float by = A.x_scales ? A.x_scales[t] : 1.f;
+    if constexpr (MODE == MM_PLAIN) {
+        finish4<MODE>(A, t, w * 64 + in, DX ? A.m : A.n, v0, gq_float4{}, by);
+        finish4<MODE>(A, t, w * 64 + 32 + in, DX ? A.m : A.n, v1, gq_float4{}, by);
+    } else {
+        finish4<MODE>(A, t, w * 32 + in, A.n, v0, v1, by);
+    }
+}
 
-template <bool DX, int MODE, int STAGE>
-__global__ void __launch_bounds__(WIDE_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) group_wide_kernel(MmArgs A, int group, int mats, int ttiles) {
+// Four wavefronts side by side; with KS = 2 four more sum the other half of the columns, and the halves meet in LDS at the end.  `parts`
+// workgroups share a tile's columns further: their sums go to `partial`, and group_join_kernel adds them up.
+template <bool DX, int MODE, int KS>
+__global__ void __launch_bounds__(WIDE_THREADS *KS) __attribute__((amdgpu_waves_per_eu(2, 2)))
+group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int parts, gq_float4 *partial) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane >> 4, l16 = lane & 15;
-    const int tile = xcd_order(blockIdx.x, gridDim.x);
+    const int kg = wave / WIDE_R, rg = wave % WIDE_R;
+    const int work = xcd_order(blockIdx.x, gridDim.x), part = work / tiles, tile = work - part * tiles;
     const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * WIDE_TOKENS;
     const long long kbs = gq_col_blocks(A.m), rbs = gq_row_blocks(A.n), n16 = rbs * GQ_ROWS;
     const long long depth = DX ? A.n : A.m;                          // summed over
     const int blocks = (int)((depth + 127) / 128), total = DX ? blocks * mats : blocks;
     const int per = GQ_COLS / group;
+    const int share = part * KS + kg, shares = parts * KS;
+    const int kb0 = (int)((long long)total * share / shares), kb1 = (int)((long long)total * (share + 1) / shares);
+    const int rounds = (total + shares - 1) / shares;                // (of the longest share: all wavefronts meet at every barrier)
 
-    // ---- the tokens' operand
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte *)smem;
-    const int es = STAGE == STAGE_E4M3 ? 1 : 2;
-    uint32_t voff[WIDE_UNITS];
-    gq_word2 held[WIDE_UNITS];                                       // e4m3: the next block's units on their way
+    // ---- the tokens' operand: 8 copies of 1 KB a wavefront and block, 4 tokens of 16 units each
+    unsigned char *const xbuf = smem + kg * 2 * WIDE_X_BYTES;
+    const uint32_t lds_x = (uint32_t)(uintptr_t)(lds_byte *)xbuf + (uint32_t)rg * 8192u;
+    const uint32_t ldb = (uint32_t)(A.ldx * 2), voff0 = (uint32_t)(rg * 32 + c) * ldb;       // of the token of copy 0
+    const int unit0 = l16 ^ c;                                                               // its unit
+    auto stage = [&](int kb, int place) {
+        const int a = DX && kb >= blocks ? 1 : 0;
+        const long long col = (long long)(kb - a * blocks) * GQ_COLS;
+        const int left = (int)min(depth - col, (long long)GQ_COLS);
+        // (rows come in whole octets; tokens past the last lie past the end of x, where zeros arrive from)
+        const LdsSource src{(uint64_t)(uintptr_t)((const uint16_t *)(a ? A.x2 : A.x) + t0 * A.ldx + col), ((A.T - 1 - t0) * A.ldx + (depth + 7) / 8 * 8 - col) * 2};
+        const int4v rs = src.rsrc();
 #pragma unroll
-    for (int i = 0; i < WIDE_UNITS; ++i) {
-        const int t = (wave * WIDE_UNITS + i) * 4 + c;               // (copies: 4 tokens of 16 units each)
-        voff[i] = (uint32_t)(min((long long)t, A.T - 1 - t0) * A.ldx * es) + (uint32_t)((l16 ^ (t & 15)) * 8 * es);
-    }
-    auto xbase = [&](int kb) -> const unsigned char * {
-        const int a = DX ? kb / blocks : 0;
-        return (const unsigned char *)(a ? A.x2 : A.x) + (t0 * A.ldx + (long long)(kb - a * blocks) * GQ_COLS) * es;
-    };
-    auto columns_left = [&](int kb) -> int { return (int)min(depth - (long long)(kb % blocks) * GQ_COLS, 128ll); };
-    auto unit_column = [&](int i) -> int { return (l16 ^ ((i * 4 + c) & 15)) * 8; };
-    auto stage = [&](int kb) {
-        const int left = columns_left(kb);
-        const uint32_t dst = lds0 + (uint32_t)(kb & 1) * WIDE_X_BYTES + (uint32_t)wave * (WIDE_X_BYTES / 4);
-        if constexpr (STAGE == STAGE_COPY) {
-            const LdsSource src{(uint64_t)(uintptr_t)xbase(kb), 0x7FFFFFFF};
-            const int4v rs = src.rsrc();
-#pragma unroll
-            for (int i = 0; i < WIDE_UNITS; ++i) copy_to_lds(dst + i * 1024, unit_column(i) < left ? voff[i] : 0x80000000u, rs);
-        } else if constexpr (STAGE == STAGE_E4M3) {
-            const unsigned char *x = xbase(kb);
-#pragma unroll
-            for (int i = 0; i < WIDE_UNITS; ++i) {
-                held[i] = gq_word2{};
-                const int over = unit_column(i) - left;
-                if (over <= -8) __builtin_memcpy(&held[i], x + voff[i], 8);
-                else if (over < 0) {
-                    uint8_t e[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) e[q] = over + q < 0 ? x[voff[i] + q] : (uint8_t)0;
-                    __builtin_memcpy(&held[i], e, 8);
-                }
-            }
-        } else {
-            const unsigned char *x = xbase(kb);
-#pragma unroll
-            for (int i = 0; i < WIDE_UNITS; ++i) {
-                gq_word4 v = {};
-                const int over = unit_column(i) - left;
-                if (over <= -8) __builtin_memcpy(&v, x + voff[i], 16);
-                else if (over < 0) {
-                    uint16_t e[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) e[q] = over + q < 0 ? ((const uint16_t *)(x + voff[i]))[q] : (uint16_t)0;
-                    __builtin_memcpy(&v, e, 16);
-                }
-                *(gq_word4 *)(smem + (dst - lds0) + i * 1024 + lane * 16) = v;
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int u = unit0 ^ 4 * (i & 3);
+            copy_to_lds(lds_x + place * WIDE_X_BYTES + i * 1024, u * 8 < left ? voff0 + (uint32_t)(4 * i) * ldb + (uint32_t)(u * 16) : 0x80000000u, rs);
         }
     };
-    auto store_held = [&](int kb) {
-        unsigned char *dst = smem + (kb & 1) * WIDE_X_BYTES + wave * (WIDE_X_BYTES / 4);
-#pragma unroll
-        for (int i = 0; i < WIDE_UNITS; ++i) *(gq_bf16x8 *)(dst + i * 1024 + lane * 16) = widen(held[i]);
-    };
 
-    // ---- the weights' operand
+    // ---- the weights' operand.  Half step s of a block: 16 columns (rows for dx) of all 64 rows (columns).
+    const int hi = lane >> 5;
     constexpr int PAIR = MODE == MM_PLAIN ? 4 : 2;                   // row blocks of a wavefront, of one matrix
-    const long long rb0 = (ob * 4 + wave) * PAIR;
-    const long long cb = min(ob * 2 + (wave >> 1), kbs - 1);         // dx: column block, and which half of it
-    const int half = wave & 1;
-    gq_word4 next[4];
-    uint32_t nscale[4];
+    const long long rb0 = (ob * WIDE_R + rg) * PAIR;
+    const long long cb = min((ob * WIDE_R + rg) >> 1, kbs - 1);           // dx: column block, and which half of it
+    const int half = rg & 1;
+    gq_word4 next[4], cur[4];        // forward: [2 row tile + p], p: columns 16 p + 8 hi of every 32; dx: two row blocks of two words each
+    // The block's scales.  Forward: [2 row tile + w]: those of words 2 w and 2 w + 1.  dx: [row / 64]: those of the two words.  They come two rows a
+    // register, [4 row tile + group] or [2 (row / 64) + group], and stay so until take_codes: anything done to them earlier would wait for them.
+    uint32_t nscale[8], cscale[4];
+    // (addresses: a wavefront's own, and 32-bit places of the lanes)
+    uint32_t wplace[2], splace[2];
+    long long rbu[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        rbu[i] = min(rb0 + (MODE == MM_PLAIN ? 2 * i : 0), rbs - 1);
+        const int second = rbu[i] + 1 < rbs ? c & 1 : 0;
+        wplace[i] = DX ? (uint32_t)(lane * 16 + 8 * half) : (uint32_t)(second * kbs) * 1024u + (uint32_t)(16 * hi + l16) * 16u;
+        splace[i] = DX ? (uint32_t)(lane & ~1) : (uint32_t)(second * 16 + (l16 & ~1)) * 2u;
+    }
     auto load_codes = [&](int kb) {
         if constexpr (DX) {
-            const int a = kb / blocks;
+            const int a = kb >= blocks ? 1 : 0;
             const long long rb = (long long)(kb - a * blocks) * 8;
-            const uint32_t *w = (const uint32_t *)A.codes[a] + (cb * 64 + lane) * 4 + 2 * half;
+            const char *w = (const char *)A.codes[a] + (rb * kbs + cb) * 1024;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 gq_word2 v = {};
-                if (rb + j < rbs) v = *(const gq_word2 *)(w + (rb + j) * kbs * 256);
+                if (rb + j < rbs) v = *(const gq_word2 *)(w + j * kbs * 1024 + wplace[0]);
                 next[j >> 1][2 * (j & 1)] = v[0];
                 next[j >> 1][2 * (j & 1) + 1] = v[1];
             }
+            const char *s = (const char *)(A.scales[a] + (cb * per + 64 * half / group) * n16 + rb * GQ_ROWS);
+            const uint32_t last = (uint32_t)min(n16 - rb * GQ_ROWS, 128ll) - 2;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)                              // word q / 2 of the half, rows q % 2 * 64 + lane
-                nscale[q] = A.scales[a][(cb * per + (64 * half + 32 * (q >> 1)) / group) * n16 + min(rb * GQ_ROWS + 64 * (q & 1) + lane, n16 - 1)];
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t row = min(splace[0] + 64u * q, last);
+                nscale[2 * q] = *(const uint32_t *)(s + row * 2);
+                if (group == 32) nscale[2 * q + 1] = *(const uint32_t *)(s + n16 * 2 + row * 2);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) next[i] = A.codes[i / PAIR][(min(rb0 + i % PAIR, rbs - 1) * kbs + kb) * 64 + lane];
-            const uint16_t *s = A.scales[c / PAIR] + min(rb0 + c % PAIR, rbs - 1) * GQ_ROWS + l16;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) nscale[q] = s[((long long)kb * per + 32 * q / group) * n16];
+            for (int i = 0; i < 2; ++i) {
+                const int m = MODE == MM_PLAIN ? 0 : i;
+                const char *w = (const char *)A.codes[m] + (rbu[i] * kbs + kb) * 1024;
+                next[2 * i] = *(const gq_word4 *)(w + wplace[i]);
+                next[2 * i + 1] = *(const gq_word4 *)(w + wplace[i] + 512);
+                const char *s = (const char *)(A.scales[m] + (long long)kb * per * n16 + rbu[i] * GQ_ROWS);
+                nscale[4 * i] = *(const uint32_t *)(s + splace[i]);
+                if (group <= 64) nscale[4 * i + 1] = *(const uint32_t *)(s + n16 * 2 + splace[i]);
+                if (group == 32) {
+                    nscale[4 * i + 2] = *(const uint32_t *)(s + n16 * 4 + splace[i]);
+                    nscale[4 * i + 3] = *(const uint32_t *)(s + n16 * 6 + splace[i]);
+                }
+            }
         }
     };
-    gq_word4 cur[4];
-    uint32_t cscale[4];
-    unsigned char *mine = smem + 2 * WIDE_X_BYTES + wave * WIDE_A_BYTES;
+    unsigned char *mine = smem + 2 * KS * WIDE_X_BYTES + wave * WIDE_A_BYTES;
     auto flip = [](int row) { return (2 * (row & 3)) ^ ((row >> 2) & 1); };    // dx: unit u of a row is at u ^ flip(row)
-    auto operands = [&](int k, gq_bf16x8 (&a)[4]) {
+    auto operands = [&](int s, gq_bf16x8 (&a)[2]) {
         if constexpr (DX) {
+            const uint32_t f = (uint32_t)__shfl((int)cscale[s >> 2], 16 * (s & 3) + l16, 64);
+            unsigned char *place = mine + (s & 1) * (WIDE_A_BYTES / 2);
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {                            // row block p / 2 of the step, word p % 2
-                const int j = 2 * k + (p >> 1), q = p & 1;
-                const float s = gq_scale((uint32_t)__shfl((int)cscale[2 * q + (j >> 2)], 16 * (j & 3) + l16, 64));
-                const int row = 16 * (p >> 1) + l16;
-                *(gq_word4 *)(mine + row * 128 + ((4 * q + c) ^ flip(row)) * 16) = weight_operand(cur[j >> 1][2 * (j & 1) + q], s);
-            }
+            for (int q = 0; q < 2; ++q)
+                *(gq_word4 *)(place + l16 * 128 + ((4 * q + c) ^ flip(l16)) * 16) =
+                    weight_operand(cur[s >> 1][2 * (s & 1) + q], q ? __uint_as_float(f & 0xFFFF0000u) : __uint_as_float(f << 16));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 8 * c + (l16 >> 2), u = 2 * i + ((l16 & 3) >> 1);
-                const gq_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(mine + row * 128 + (u ^ flip(row)) * 16 + (l16 & 1) * 8));
-                const gq_short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(mine + (row + 4) * 128 + (u ^ flip(row + 4)) * 16 + (l16 & 1) * 8));
-                a[i] = __builtin_bit_cast(gq_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            for (int i = 0; i < 2; ++i) {
+                // 16 lanes read 4 rows of 16 columns and get 4 rows of one column each; a lane's operand: column lane % 32, rows 8 hi .. 8 hi + 7
+                const int row = 8 * hi + (l16 >> 2), u = 4 * i + 2 * (c & 1) + ((l16 & 3) >> 1);
+                const gq_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(place + row * 128 + (u ^ flip(row)) * 16 + (l16 & 1) * 8));
+                const gq_short4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(place + (row + 4) * 128 + (u ^ flip(row + 4)) * 16 + (l16 & 1) * 8));
+                a[i] = __builtin_bit_cast(gq_bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         } else {
+            const int k = s >> 1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float s = gq_scale((uint32_t)__shfl((int)cscale[k], 16 * i + l16, 64));
-                a[i] = __builtin_bit_cast(gq_bf16x8, weight_operand(cur[i][k], s));
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t f = cscale[2 * i + (k >> 1)];
+                a[i] = __builtin_bit_cast(gq_bf16x8, weight_operand(cur[2 * i + (s & 1)][k], k & 1 ? __uint_as_float(f & 0xFFFF0000u) : __uint_as_float(f << 16)));
+            }
+        }
+    };
+    // the next block's codes have come (and all copies with them)
+    auto take_codes = [&]() {
+        asm volatile("s_waitcnt vmcnt(0)"
+                     : "+v"(next[0]), "+v"(next[1]), "+v"(next[2]), "+v"(next[3]), "+v"(nscale[0]), "+v"(nscale[1]), "+v"(nscale[2]), "+v"(nscale[3]),
+                       "+v"(nscale[4]), "+v"(nscale[5]), "+v"(nscale[6]), "+v"(nscale[7])
+                     :
+                     : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cur[i] = next[i];
+        const uint32_t pick = lane & 1 ? 0x03020302u : 0x01000100u, both = lane & 1 ? 0x07060302u : 0x05040100u;       // the lane's row; of two registers
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if constexpr (DX) {
+                cscale[i] = group == 32 ? __builtin_amdgcn_perm(nscale[2 * i + 1], nscale[2 * i], both) : __builtin_amdgcn_perm(0u, nscale[2 * i], pick);
+            } else if (group == 128) {
+                cscale[2 * i] = cscale[2 * i + 1] = __builtin_amdgcn_perm(0u, nscale[4 * i], pick);
+            } else if (group == 64) {
+                cscale[2 * i] = __builtin_amdgcn_perm(0u, nscale[4 * i], pick);
+                cscale[2 * i + 1] = __builtin_amdgcn_perm(0u, nscale[4 * i + 1], pick);
+            } else {
+                cscale[2 * i] = __builtin_amdgcn_perm(nscale[4 * i + 1], nscale[4 * i], both);
+                cscale[2 * i + 1] = __builtin_amdgcn_perm(nscale[4 * i + 3], nscale[4 * i + 2], both);
             }
         }
     };
 
-    gq_float4 acc[WIDE_RT][WIDE_TT] = {};
-    stage(0);
-    load_codes(0);
-    if constexpr (STAGE == STAGE_E4M3) store_held(0);
-    for (int kb = 0; kb < total; ++kb) {
-        // this block's copies have landed, its codes too, and everybody is done with the block before, whose place the next one takes
+    floatx16 acc[2][4] = {};
+    gq_bf16x8 a[2][2], b[2][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            cur[i] = next[i];
-            cscale[i] = nscale[i];
-        }
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier"
-                     : "+v"(cur[0]), "+v"(cur[1]), "+v"(cur[2]), "+v"(cur[3]), "+v"(cscale[0]), "+v"(cscale[1]), "+v"(cscale[2]), "+v"(cscale[3])
-                     :
-                     : "memory");
-        if (kb + 1 < total) {
-            stage(kb + 1);
+    for (int i = 0; i < 4; ++i) {
+        next[i] = gq_word4{};
+        nscale[i] = nscale[4 + i] = 0;
+    }
+    if (kb0 < kb1) {
+        stage(kb0, 0);
+        load_codes(kb0);
+    }
+    take_codes();
+    operands(0, a[0]);
+    for (int r = 0; r < rounds; ++r) {
+        const int kb = kb0 + r, now = r & 1;                         // block, and which of the two places in LDS it is in
+        // this block's copies have landed, and everybody is done with the block before, whose place the next one takes
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (kb >= kb1) continue;                                     // (a share that is one block shorter)
+        if (kb + 1 < kb1) {
+            stage(kb + 1, now ^ 1);
             load_codes(kb + 1);
         }
-        const unsigned char *xb = smem + (kb & 1) * WIDE_X_BYTES + l16 * 256;
+        const unsigned char *xb = xbuf + now * WIDE_X_BYTES + (lane & 31) * (GQ_COLS * 2);
+        auto read_x = [&](int s, gq_bf16x8 (&v)[4]) {
+            const int place = (2 * s + hi) ^ l16;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            gq_bf16x8 a[4];
-            operands(k, a);
+            for (int j = 0; j < 4; ++j) v[j] = *(const gq_bf16x8 *)(xb + j * 32 * GQ_COLS * 2 + place * 16);
+        };
+        read_x(0, b[0]);
 #pragma unroll
-            for (int j = 0; j < WIDE_TT; ++j) {
-                const gq_bf16x8 b = *(const gq_bf16x8 *)(xb + j * 4096 + (((4 * k + c) ^ l16) << 4));
-#pragma unroll
-                for (int i = 0; i < WIDE_RT; ++i) acc[i][j] = mfma(a[i], b, acc[i][j]);
+        for (int s = 0; s < 8; ++s) {
+            if (s < 7) {
+                read_x(s + 1, b[(s + 1) & 1]);
+                operands(s + 1, a[(s + 1) & 1]);
+            } else {
+                take_codes();
+                operands(0, a[0]);
             }
-        }
-        if constexpr (STAGE == STAGE_E4M3) {
-            if (kb + 1 < total) store_held(kb + 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i], b[s & 1][j], acc[i][j], 0, 0, 0);
+            if constexpr (!DX) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (q < 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
+    int j0 = 0, j1 = 4;
+    if constexpr (KS == 2) {                                         // each four give half of their sums and finish the others
+        floatx16 *give = (floatx16 *)smem + (size_t)wave * 256 + lane;
+        const floatx16 *take = (const floatx16 *)smem + (size_t)(wave ^ WIDE_R) * 256 + lane;
+        __syncthreads();
 #pragma unroll
-    for (int j = 0; j < WIDE_TT; ++j) {
-        const long long t = t0 + 16 * j + l16;
-        if (t >= A.T) continue;
-        const float by = STAGE == STAGE_E4M3 ? A.x_scales[t] : 1.f;
-        if constexpr (DX) {
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) finish4<MM_PLAIN>(A, t, (ob * 4 + wave) * 64 + 16 * i + 4 * c, A.m, acc[i][j], acc[i][j], 1.f);
+            for (int j = 0; j < 2; ++j) give[(i * 2 + j) * 64] = kg == 0 ? acc[i][j + 2] : acc[i][j];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const floatx16 o = take[(i * 2 + j) * 64];
+                if (kg == 0) acc[i][j] += o;
+                else acc[i][j + 2] += o;
+            }
+        j0 = 2 * kg;
+        j1 = j0 + 2;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (j < j0 || j >= j1) continue;
+        auto four = [&](int i, int q) { return gq_float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}; };
+        if (parts > 1) {
+            gq_float4 *p = partial + ((((size_t)part * tiles + tile) * WIDE_R + rg) * 4 + j) * 512 + lane;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) p[(2 * q + i) * 64] = four(i, q);
         } else {
 #pragma unroll
-            for (int i = 0; i < PAIR; ++i) finish4<MODE>(A, t, (rb0 + i) * GQ_ROWS + 4 * c, A.n, acc[i][j], acc[MODE == MM_PLAIN ? i : i + PAIR][j], by);
+            for (int q = 0; q < 4; ++q) wide_finish<DX, MODE>(A, ob * WIDE_R + rg, t0 + 32 * j + (lane & 31), 8 * q + 4 * hi, four(0, q), four(1, q));
         }
     }
+}
+
+// The parts of a tile added up in their order, and finished: one wavefront for 32 tokens and 16 of a wavefront's rows.
+template <bool DX, int MODE>
+__global__ void __launch_bounds__(256) group_join_kernel(MmArgs A, int ttiles, int tiles, int parts, const gq_float4 *__restrict__ partial) {
+    const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const int tile = blockIdx.x / (4 * WIDE_R), rg = blockIdx.x / 4 % WIDE_R, j = blockIdx.x % 4;
+    const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * WIDE_TOKENS;
+    const gq_float4 *p = partial + (((size_t)tile * WIDE_R + rg) * 4 + j) * 512 + 2 * q * 64 + lane;
+    const size_t step = (size_t)tiles * WIDE_R * 4 * 512;
+    gq_float4 v0 = p[0], v1 = p[64];
+    for (int i = 1; i < parts; ++i) {
+        v0 += p[i * step];
+        v1 += p[i * step + 64];
+    }
+    wide_finish<DX, MODE>(A, ob * WIDE_R + rg, t0 + 32 * j + (lane & 31), 8 * q + 4 * (lane >> 5), v0, v1);
+}
+
+// x as the tiles take it: bfloat16, rows of `columns` values on 16-byte borders.  (In the tiles themselves the conversion of e4m3 through registers
+// cost 40 % of their time, for want of registers; this pass, bound by the 3 bytes a value, costs 4 % of it.)
+template <int XT>
+__global__ void __launch_bounds__(256) group_widen_kernel(const void *x, long long ldx, long long T, int m, int columns, uint16_t *out) {
+    const long long octets = columns / 8, at = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= T * octets) return;
+    const long long t = at / octets, col = (at - t * octets) * 8;
+    *(gq_bf16x8 *)(out + t * columns + col) = load_x<XT, false>(x, t * ldx, col, m);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -430,36 +524,88 @@ bool all_on(int64_t border, std::initializer_list<const void *> ps) {
     return true;
 }
 
-template <bool DX, int MODE>
-skim_status launch_wide(skim_ctx *ctx, const MmArgs &A, int group, int x_type, int mats) {
-    const int64_t out = DX ? A.m : A.n, per = MODE == MM_PLAIN ? 256 : 128;
-    const int64_t ttiles = (A.T + WIDE_TOKENS - 1) / WIDE_TOKENS, tiles = (out + per - 1) / per * ttiles, depth = DX ? A.n : A.m;
-    if (tiles > 0x7fffffff || A.ldx >= (1 << 23) || depth > (1 << 24))
-        SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens of row stride %lld are too many for one call", A.T, A.ldx);
-    const size_t lds = 2 * WIDE_X_BYTES + (DX ? 4 * WIDE_A_BYTES : 0);
-    const bool copy = x_type == SKIM_BF16 && depth % 8 == 0 && A.ldx % 8 == 0 && all_on(16, {A.x, A.x2});
-    auto go = [&](auto stage) -> hipError_t {
-        auto *k = &group_wide_kernel<DX, MODE, decltype(stage)::value>;
-        hipError_t e = hipSuccess;
-        if (lds > 64 * 1024) e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e == hipSuccess) hipLaunchKernelGGL(k, dim3((unsigned)tiles), dim3(WIDE_THREADS), lds, ctx->stream, A, group, mats, (int)ttiles);
-        return e;
-    };
-    hipError_t e;
-    if (copy) e = go(std::integral_constant<int, STAGE_COPY>{});
-    else if (x_type == SKIM_BF16) e = go(std::integral_constant<int, STAGE_BF16>{});
-    else if constexpr (!DX) e = go(std::integral_constant<int, STAGE_E4M3>{});
-    else SKIM_FAIL(ctx, SKIM_ERR_ARG, "gradients are bfloat16");
-    SKIM_HIP(ctx, e);
+// How the tiles of a product are shared out: `ks` times four wavefronts a workgroup, `parts` workgroups a tile.
+struct WidePlan {
+    int64_t ttiles, tiles;
+    int ks, parts;
+    size_t scratch() const { return parts > 1 ? (size_t)tiles * parts * WIDE_R * 4 * 512 * sizeof(gq_float4) : 0; }
+};
+WidePlan wide_plan(const skim_ctx *ctx, int64_t out, int64_t per, int64_t blocks, int64_t T) {
+    WidePlan p;
+    p.ttiles = (T + WIDE_TOKENS - 1) / WIDE_TOKENS;
+    p.tiles = (out + per - 1) / per * p.ttiles;
+    p.ks = p.tiles <= ctx->num_cu && blocks >= 4 ? 2 : 1;
+    p.parts = 1;
+    if (p.ks == 2) p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ctx->num_cu / p.tiles, blocks / 8));
+    return p;
+}
+
+// Whether the tiles can copy rows of x as they are.
+bool wide_takes(const void *x, int x_type, int64_t ldx, int64_t depth) {
+    return x_type == SKIM_BF16 && depth % 8 == 0 && ldx % 8 == 0 && ldx < (1 << 23) && all_on(16, {x});
+}
+int64_t wide_columns(int64_t depth) { return (depth + 7) / 8 * 8; }
+size_t widened_bytes(int64_t depth, int64_t T) { return ((size_t)wide_columns(depth) * T * 2 + 255) / 256 * 256; }
+
+skim_status widen_x(skim_ctx *ctx, const void *x, int x_type, int64_t ldx, int64_t T, int64_t depth, void *out) {
+    const int64_t columns = wide_columns(depth), groups = (T * (columns / 8) + 255) / 256;
+    if (groups > 0x7fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens of %lld values are too many for one call", (long long)T, (long long)depth);
+    if (x_type == SKIM_BF16)
+        hipLaunchKernelGGL(group_widen_kernel<SKIM_BF16>, dim3((unsigned)groups), dim3(256), 0, ctx->stream, x, (long long)ldx, (long long)T, (int)depth, (int)columns,
+                           (uint16_t *)out);
+    else
+        hipLaunchKernelGGL(group_widen_kernel<SKIM_E4M3>, dim3((unsigned)groups), dim3(256), 0, ctx->stream, x, (long long)ldx, (long long)T, (int)depth, (int)columns,
+                           (uint16_t *)out);
     SKIM_HIP(ctx, hipGetLastError());
     return SKIM_OK;
 }
 
+template <bool DX, int MODE>
+skim_status launch_wide(skim_ctx *ctx, MmArgs A, int group, int x_type, int mats, void *scratch, size_t scratch_bytes) {
+    const int64_t depth = DX ? A.n : A.m;
+    char *room = (char *)scratch;
+    if (!wide_takes(A.x, x_type, A.ldx, depth) || (mats == 2 && !wide_takes(A.x2, x_type, A.ldx, depth))) {
+        const size_t each = widened_bytes(depth, A.T), need = each * mats;
+        if (need > scratch_bytes)
+            SKIM_FAIL(ctx, SKIM_ERR_WORKSPACE, "%lld tokens of this type, stride or alignment need %zu bytes of scratch, %zu given", A.T, need, scratch_bytes);
+        skim_status st;
+        if ((st = widen_x(ctx, A.x, x_type, A.ldx, A.T, depth, room)) != SKIM_OK) return st;
+        if (mats == 2 && (st = widen_x(ctx, A.x2, x_type, A.ldx, A.T, depth, room + each)) != SKIM_OK) return st;
+        A.x = room;
+        A.x2 = room + each;
+        A.ldx = wide_columns(depth);
+        room += need;
+        scratch_bytes -= need;
+    }
+    WidePlan p = wide_plan(ctx, DX ? A.m : A.n, MODE == MM_PLAIN ? 256 : 128, (depth + 127) / 128 * mats, A.T);
+    if (p.scratch() > scratch_bytes) p.parts = 1;
+    if (p.tiles > 0x3fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens are too many for one call", A.T);
+    const size_t lds = p.ks * (2 * WIDE_X_BYTES + (DX ? 4 * WIDE_A_BYTES : 0));
+    auto go = [&](auto split) -> hipError_t {
+        constexpr int KS = decltype(split)::value;
+        auto *k = &group_wide_kernel<DX, MODE, KS>;
+        hipError_t e = hipSuccess;
+        if (lds > 64 * 1024) e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e == hipSuccess)
+            hipLaunchKernelGGL(k, dim3((unsigned)(p.tiles * p.parts)), dim3(WIDE_THREADS * KS), lds, ctx->stream, A, group, mats, (int)p.ttiles, (int)p.tiles, p.parts,
+                               (gq_float4 *)room);
+        return e;
+    };
+    SKIM_HIP(ctx, p.ks == 1 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{}));
+    SKIM_HIP(ctx, hipGetLastError());
+    if (p.parts > 1) {
+        hipLaunchKernelGGL((group_join_kernel<DX, MODE>), dim3((unsigned)(p.tiles * WIDE_R * 4)), dim3(256), 0, ctx->stream, A, (int)p.ttiles, (int)p.tiles, p.parts,
+                           (const gq_float4 *)room);
+        SKIM_HIP(ctx, hipGetLastError());
+    }
+    return SKIM_OK;
+}
+
 template <int MODE>
-skim_status launch_forward(skim_ctx *ctx, MmArgs A, int group, int x_type) {
+skim_status launch_forward(skim_ctx *ctx, MmArgs A, int group, int x_type, void *scratch, size_t scratch_bytes) {
     A.quads = A.n % 4 == 0 && all_on(16, {A.y, A.dgate, A.dup}) && (!A.da || (A.ldda % 4 == 0 && all_on(8, {A.da})));
     constexpr int MATS = MODE == MM_PLAIN ? 1 : 2;
-    if (A.T >= WIDE_FROM) return launch_wide<false, MODE>(ctx, A, group, x_type, 1);
+    if (A.T >= WIDE_FROM) return launch_wide<false, MODE>(ctx, A, group, x_type, 1, scratch, scratch_bytes);
     const int nt = A.T <= 16 ? 1 : A.T <= 32 ? 2 : 4;
     const int64_t chunks = (A.T + 16 * nt - 1) / (16 * nt), groups = gq_row_blocks(A.n) * chunks;
     if (groups > 0x7fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens on %lld rows are too many for one call", A.T, A.n);
@@ -489,9 +635,9 @@ skim_status launch_forward(skim_ctx *ctx, MmArgs A, int group, int x_type) {
     return SKIM_OK;
 }
 
-skim_status launch_dx(skim_ctx *ctx, MmArgs A, int group, int mats) {
+skim_status launch_dx(skim_ctx *ctx, MmArgs A, int group, int mats, void *scratch, size_t scratch_bytes) {
     A.quads = A.m % 4 == 0 && all_on(16, {A.y});
-    return launch_wide<true, MM_PLAIN>(ctx, A, group, SKIM_BF16, mats);
+    return launch_wide<true, MM_PLAIN>(ctx, A, group, SKIM_BF16, mats, scratch, scratch_bytes);
 }
 
 skim_status check_x(skim_ctx *ctx, const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, int64_t m, const char *who) {
@@ -499,6 +645,11 @@ skim_status check_x(skim_ctx *ctx, const void *x, int x_type, int64_t ldx, const
     if (T < 0 || T > 0x7fffffff || ldx < m) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%s: bad shape T=%lld m=%lld ldx=%lld", who, (long long)T, (long long)m, (long long)ldx);
     if (T > 0 && (!x || (x_type == SKIM_E4M3) != (x_scales != nullptr)))
         SKIM_FAIL(ctx, SKIM_ERR_ARG, "%s: x must not be NULL, and x_scales is given with e4m3 and only then", who);
+    return SKIM_OK;
+}
+
+skim_status check_scratch(skim_ctx *ctx, const void *scratch, size_t bytes, const char *who) {
+    if ((bytes && !scratch) || ((uintptr_t)scratch & 15)) SKIM_FAIL(ctx, SKIM_ERR_ARG, "%s: scratch must be 16-byte aligned, and not NULL where it has a size", who);
     return SKIM_OK;
 }
 
@@ -521,37 +672,49 @@ MmArgs matrix_args(const uint32_t *codes, const uint16_t *scales, const uint32_t
 
 }  // namespace
 
+extern "C" size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T) {
+    if (!ctx || n < 1 || n > SKIM_GROUP_MAX || m < 1 || m > SKIM_GROUP_MAX || T < 1 || T > 0x7fffffff) return 0;
+    const int64_t over_m = (m + 127) / 128, over_n = (n + 127) / 128;
+    // forward: x in another type or alignment, and the partial sums; to the input: the same for two gradients whose rows are not multiples of 8
+    const size_t to_out = std::max(wide_plan(ctx, n, 256, over_m, T).scratch(), wide_plan(ctx, n, 128, over_m, T).scratch());
+    const size_t to_in = std::max(wide_plan(ctx, m, 256, over_n, T).scratch(), wide_plan(ctx, m, 256, 2 * over_n, T).scratch());
+    return std::max(T < WIDE_FROM ? (size_t)0 : widened_bytes(m, T) + to_out, (n % 8 ? 2 : 1) * widened_bytes(n, T) + to_in);
+}
+
 extern "C" skim_status skim_group_matmul(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
-                                         const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, void *y, int y_type) {
+                                         const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, void *y, int y_type,
+                                         void *scratch, size_t scratch_bytes) {
     skim_status st = skim_enter(ctx);
     if (st != SKIM_OK) return st;
     const char *who = "skim_group_matmul";
     if ((st = skim_group_check(ctx, codes, scales_bf16, n, m, group, who)) != SKIM_OK) return st;
     if ((st = check_x(ctx, x, x_type, ldx, x_scales, T, m, who)) != SKIM_OK) return st;
     if ((st = check_out(ctx, y, y_type, T, who)) != SKIM_OK) return st;
+    if ((st = check_scratch(ctx, scratch, scratch_bytes, who)) != SKIM_OK) return st;
     if (T == 0) return SKIM_OK;
     MmArgs A = matrix_args(codes, scales_bf16, nullptr, nullptr, n, m);
     A.x = x, A.ldx = ldx, A.x_scales = x_scales, A.T = T, A.y = y, A.y_f32 = y_type == SKIM_F32;
-    return launch_forward<MM_PLAIN>(ctx, A, group, x_type);
+    return launch_forward<MM_PLAIN>(ctx, A, group, x_type, scratch, scratch_bytes);
 }
 
 extern "C" skim_status skim_group_matmul_dx(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
-                                            const uint16_t *dy_bf16, int64_t lddy, int64_t T, void *dx, int dx_type) {
+                                            const uint16_t *dy_bf16, int64_t lddy, int64_t T, void *dx, int dx_type, void *scratch, size_t scratch_bytes) {
     skim_status st = skim_enter(ctx);
     if (st != SKIM_OK) return st;
     const char *who = "skim_group_matmul_dx";
     if ((st = skim_group_check(ctx, codes, scales_bf16, n, m, group, who)) != SKIM_OK) return st;
     if ((st = check_x(ctx, dy_bf16, SKIM_BF16, lddy, nullptr, T, n, who)) != SKIM_OK) return st;
     if ((st = check_out(ctx, dx, dx_type, T, who)) != SKIM_OK) return st;
+    if ((st = check_scratch(ctx, scratch, scratch_bytes, who)) != SKIM_OK) return st;
     if (T == 0) return SKIM_OK;
     MmArgs A = matrix_args(codes, scales_bf16, nullptr, nullptr, n, m);
     A.x = dy_bf16, A.ldx = lddy, A.T = T, A.y = dx, A.y_f32 = dx_type == SKIM_F32;
-    return launch_dx(ctx, A, group, 1);
+    return launch_dx(ctx, A, group, 1, scratch, scratch_bytes);
 }
 
 extern "C" skim_status skim_group_glu(skim_ctx *ctx, const uint32_t *gate_codes, const uint16_t *gate_scales, const uint32_t *up_codes,
                                       const uint16_t *up_scales, int64_t n, int64_t m, int group, const void *x, int x_type, int64_t ldx,
-                                      const float *x_scales, int64_t T, void *a, int a_type) {
+                                      const float *x_scales, int64_t T, void *a, int a_type, void *scratch, size_t scratch_bytes) {
     skim_status st = skim_enter(ctx);
     if (st != SKIM_OK) return st;
     const char *who = "skim_group_glu";
@@ -559,16 +722,17 @@ extern "C" skim_status skim_group_glu(skim_ctx *ctx, const uint32_t *gate_codes,
     if ((st = skim_group_check(ctx, up_codes, up_scales, n, m, group, who)) != SKIM_OK) return st;
     if ((st = check_x(ctx, x, x_type, ldx, x_scales, T, m, who)) != SKIM_OK) return st;
     if ((st = check_out(ctx, a, a_type, T, who)) != SKIM_OK) return st;
+    if ((st = check_scratch(ctx, scratch, scratch_bytes, who)) != SKIM_OK) return st;
     if (T == 0) return SKIM_OK;
     MmArgs A = matrix_args(gate_codes, gate_scales, up_codes, up_scales, n, m);
     A.x = x, A.ldx = ldx, A.x_scales = x_scales, A.T = T, A.y = a, A.y_f32 = a_type == SKIM_F32;
-    return launch_forward<MM_GLU>(ctx, A, group, x_type);
+    return launch_forward<MM_GLU>(ctx, A, group, x_type, scratch, scratch_bytes);
 }
 
 extern "C" skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *gate_codes, const uint16_t *gate_scales, const uint32_t *up_codes,
                                                const uint16_t *up_scales, int64_t n, int64_t m, int group, const void *x, int x_type,
                                                int64_t ldx, const float *x_scales, int64_t T, const uint16_t *da_bf16, int64_t ldda,
-                                               uint16_t *dgate_bf16, uint16_t *dup_bf16, void *dx, int dx_type) {
+                                               uint16_t *dgate_bf16, uint16_t *dup_bf16, void *dx, int dx_type, void *scratch, size_t scratch_bytes) {
     skim_status st = skim_enter(ctx);
     if (st != SKIM_OK) return st;
     const char *who = "skim_group_glu_backward";
@@ -577,11 +741,13 @@ extern "C" skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *ga
     if ((st = check_x(ctx, x, x_type, ldx, x_scales, T, m, who)) != SKIM_OK) return st;
     if ((st = check_x(ctx, da_bf16, SKIM_BF16, ldda, nullptr, T, n, who)) != SKIM_OK) return st;
     if (dx_type != SKIM_BF16 && dx_type != SKIM_F32) SKIM_FAIL(ctx, SKIM_ERR_ARG, "%s: the result's type %d is neither SKIM_BF16 nor SKIM_F32", who, dx_type);
+    if ((st = check_scratch(ctx, scratch, scratch_bytes, who)) != SKIM_OK) return st;
     if (T == 0) return SKIM_OK;
-    if (!dgate_bf16 || !dup_bf16) SKIM_FAIL(ctx, SKIM_ERR_ARG, "%s: dgate and dup must not be NULL", who);
+    if (!dgate_bf16 || !dup_bf16 || !all_on(16, {dgate_bf16, dup_bf16}))
+        SKIM_FAIL(ctx, SKIM_ERR_ARG, "%s: dgate and dup must not be NULL, and 16-byte aligned", who);
     MmArgs A = matrix_args(gate_codes, gate_scales, up_codes, up_scales, n, m);
     A.x = x, A.ldx = ldx, A.x_scales = x_scales, A.T = T, A.da = da_bf16, A.ldda = ldda, A.dgate = dgate_bf16, A.dup = dup_bf16;
-    if ((st = launch_forward<MM_GLU_BACK>(ctx, A, group, x_type)) != SKIM_OK || !dx) return st;
-    A.x = dgate_bf16, A.x2 = dup_bf16, A.ldx = n, A.y = dx, A.y_f32 = dx_type == SKIM_F32;
-    return launch_dx(ctx, A, group, 2);
+    if ((st = launch_forward<MM_GLU_BACK>(ctx, A, group, x_type, scratch, scratch_bytes)) != SKIM_OK || !dx) return st;
+    A.x = dgate_bf16, A.x2 = dup_bf16, A.ldx = n, A.x_scales = nullptr, A.y = dx, A.y_f32 = dx_type == SKIM_F32;
+    return launch_dx(ctx, A, group, 2, scratch, scratch_bytes);
 }

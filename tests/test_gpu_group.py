@@ -151,10 +151,10 @@ def test_sizes_of_the_format(lib):
 def test_calls_without_a_context_are_refused(lib):
     assert lib.skim_group_quantize(None, None, 1, 1, 1, 128, None, None) == -1
     assert lib.skim_group_unpack(None, None, None, 1, 1, 128, None) == -1
-    assert lib.skim_group_matmul(None, None, None, 1, 1, 128, None, 1, 1, None, 1, None, 1) == -1
-    assert lib.skim_group_matmul_dx(None, None, None, 1, 1, 128, None, 1, 1, None, 1) == -1
-    assert lib.skim_group_glu(None, None, None, None, None, 1, 1, 128, None, 1, 1, None, 1, None, 1) == -1
-    assert lib.skim_group_glu_backward(None, None, None, None, None, 1, 1, 128, None, 1, 1, None, 1, None, 1, None, None, None, 1) == -1
+    assert lib.skim_group_matmul(None, None, None, 1, 1, 128, None, 1, 1, None, 1, None, 1, None, 0) == -1
+    assert lib.skim_group_matmul_dx(None, None, None, 1, 1, 128, None, 1, 1, None, 1, None, 0) == -1
+    assert lib.skim_group_glu(None, None, None, None, None, 1, 1, 128, None, 1, 1, None, 1, None, 1, None, 0) == -1
+    assert lib.skim_group_glu_backward(None, None, None, None, None, 1, 1, 128, None, 1, 1, None, 1, None, 1, None, None, None, 1, None, 0) == -1
     assert lib.skim_rms_norm(None, None, 1, None, 0, 1, None, 1e-6, 1, 1, None, None, None, None, None) == -1
     assert lib.skim_rms_norm_backward(None, None, 1, None, 1, None, 0, 1, None, None, 1, 1, None, None, None, 0) == -1
     assert lib.skim_rms_norm_scratch_bytes(None, 4, 4) == 0
@@ -233,7 +233,7 @@ def test_quantize_of_large_and_small_weights(ctx):
 
 
 PRODUCTS = [(1, 1, 1, 32), (1, 16, 128, 128), (1, 300, 1000, 64), (2, 17, 129, 32), (15, 33, 96, 32), (16, 64, 512, 128), (17, 50, 513, 64),
-            (33, 129, 640, 128), (64, 256, 256, 32), (65, 100, 384, 64), (130, 272, 1100, 128), (300, 513, 520, 128)]
+            (33, 129, 640, 128), (64, 256, 256, 32), (65, 100, 384, 64), (130, 272, 1100, 128), (300, 513, 520, 128), (129, 130, 5000, 64), (70, 2100, 300, 128)]
 
 
 @pytest.mark.gpu
@@ -573,23 +573,25 @@ def test_refusals(ctx, gpu_lib):
     lib, h = ctx.lib, ctx.h
     ARG, SHAPE, WS = -1, -2, -4
     mm = lib.skim_group_matmul
-    assert mm(h, None, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 1) == ARG
-    assert mm(h, cp + 4, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 1) == ARG and b"aligned" in lib.skim_last_error(h)
-    assert mm(h, cp, sp, 32, 128, 96, xp, 1, 128, None, 4, yp, 1) == ARG
-    assert mm(h, cp, sp, 0, 128, 128, xp, 1, 128, None, 4, yp, 1) == SHAPE
-    assert mm(h, cp, sp, 1 << 24, 1 << 24, 128, xp, 1, 1 << 24, None, 4, yp, 1) == SHAPE
-    assert mm(h, cp, sp, 32, 128, 128, xp, 0, 128, None, 4, yp, 1) == ARG
-    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 127, None, 4, yp, 1) == SHAPE
-    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, -1, yp, 1) == SHAPE
-    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, fp, 4, yp, 1) == ARG
-    assert mm(h, cp, sp, 32, 128, 128, qp, 2, 128, None, 4, yp, 1) == ARG
-    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 2) == ARG
-    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, None, 1) == ARG
+    assert mm(h, None, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 1, None, 0) == ARG
+    assert mm(h, cp + 4, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 1, None, 0) == ARG and b"aligned" in lib.skim_last_error(h)
+    assert mm(h, cp, sp, 32, 128, 96, xp, 1, 128, None, 4, yp, 1, None, 0) == ARG
+    assert mm(h, cp, sp, 0, 128, 128, xp, 1, 128, None, 4, yp, 1, None, 0) == SHAPE
+    assert mm(h, cp, sp, 1 << 24, 1 << 24, 128, xp, 1, 1 << 24, None, 4, yp, 1, None, 0) == SHAPE
+    assert mm(h, cp, sp, 32, 128, 128, xp, 0, 128, None, 4, yp, 1, None, 0) == ARG
+    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 127, None, 4, yp, 1, None, 0) == SHAPE
+    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, -1, yp, 1, None, 0) == SHAPE
+    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, fp, 4, yp, 1, None, 0) == ARG
+    assert mm(h, cp, sp, 32, 128, 128, qp, 2, 128, None, 4, yp, 1, None, 0) == ARG
+    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 2, None, 0) == ARG
+    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, None, 1, None, 0) == ARG
+    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 1, None, 64) == ARG
+    assert mm(h, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 1, xp + 8, 64) == ARG and b"scratch" in lib.skim_last_error(h)
     dx = lib.skim_group_matmul_dx
-    assert dx(h, cp, sp, 32, 128, 128, None, 32, 4, xp, 1) == ARG
-    assert dx(h, cp, sp, 32, 128, 128, yp, 31, 4, xp, 1) == SHAPE
-    assert lib.skim_group_glu(h, cp, sp, cp, None, 32, 128, 128, xp, 1, 128, None, 4, yp, 1) == ARG
-    assert lib.skim_group_glu_backward(h, cp, sp, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 32, None, yp, None, 1) == ARG
+    assert dx(h, cp, sp, 32, 128, 128, None, 32, 4, xp, 1, None, 0) == ARG
+    assert dx(h, cp, sp, 32, 128, 128, yp, 31, 4, xp, 1, None, 0) == SHAPE
+    assert lib.skim_group_glu(h, cp, sp, cp, None, 32, 128, 128, xp, 1, 128, None, 4, yp, 1, None, 0) == ARG
+    assert lib.skim_group_glu_backward(h, cp, sp, cp, sp, 32, 128, 128, xp, 1, 128, None, 4, yp, 32, None, yp, None, 1, None, 0) == ARG
     assert lib.skim_group_quantize(h, big.data_ptr(), 4, 128, 127, 128, cp, sp) == SHAPE
     assert lib.skim_group_quantize(h, None, 4, 128, 128, 128, cp, sp) == ARG
     assert lib.skim_group_unpack(h, cp, sp, 4, 128, 128, None) == ARG
