@@ -317,10 +317,13 @@ skim_status skim_group_unpack(skim_ctx *ctx, const uint32_t *codes, const uint16
  * skim_rms_norm writes).  Row strides ldx >= m, lddy >= n in elements; any alignment, but rows on 16-byte borders (8-byte ones for
  * e4m3) whose length is a multiple of 8 are read faster.  Results: SKIM_BF16 or SKIM_F32, dense, apart from all inputs.
  * Operands are exact and sums float32; a result is rounded once, to its type.  What x holds behind a row's m columns is not used.
- * scratch (dev, 16-byte aligned; NULL with 0 bytes = none): where the results have few tiles, several compute units share one, and their sums
- * meet there; skim_group_scratch_bytes(ctx, n, m, T) bytes (0 for most calls, at most 32 MB) are enough for any call of this section
- * on these sizes, with fewer it is slower.  The order of the sums, and so their last digits, depend on it. */
-size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T);
+ * scratch (dev, 16-byte aligned; NULL with 0 bytes = none): skim_group_scratch_bytes(ctx, n, m, T, gradients) bytes, gradients = 0 for
+ * skim_group_matmul and skim_group_glu, 1 for skim_group_matmul_dx, 2 for skim_group_glu_backward (n x m: the matrices; 0 for arguments that
+ * the calls reject, and for few tokens forward).  It takes x in bfloat16 where rows come in e4m3 or off the 16-byte borders, without room for which
+ * calls on more than 64 tokens and gradients are refused (SKIM_ERR_WORKSPACE); and partial sums, up to 32 MB, where the results have few tiles and
+ * several compute units share one: without room for them the call is slower.  The order of the sums, and so their last digits, depend on
+ * that. */
+size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients);
 skim_status skim_group_matmul(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
                               const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, void *y, int y_type,
                               void *scratch, size_t scratch_bytes);

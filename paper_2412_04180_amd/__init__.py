@@ -102,7 +102,7 @@ def load_library():
         lib.skim_group_scale_entries.restype = i64
         lib.skim_group_quantize.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp]
         lib.skim_group_unpack.argtypes = [vp, vp, vp, i64, i64, i32, vp]
-        lib.skim_group_scratch_bytes.argtypes = [vp, i64, i64, i64]
+        lib.skim_group_scratch_bytes.argtypes = [vp, i64, i64, i64, i32]
         lib.skim_group_scratch_bytes.restype = C.c_size_t
         lib.skim_group_matmul.argtypes = [vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, vp, C.c_size_t]
         lib.skim_group_matmul_dx.argtypes = [vp, vp, vp, i64, i64, i32, vp, i64, i64, vp, i32, vp, C.c_size_t]
@@ -455,11 +455,11 @@ class Context:
         return out
 
     def _group_pointers(self, gq):
-        codes, scales = gq["codes"], gq["scales"]
+        codes, scales, n, m, group = gq["codes"], gq["scales"], gq["n"], gq["m"], gq["group"]
         assert codes.dtype == self.torch.int32 and scales.dtype == self.torch.bfloat16 and codes.is_contiguous() and scales.is_contiguous()
-        assert codes.device == self.device and scales.device == self.device
-        n, m, group = gq["n"], gq["m"], gq["group"]
-        assert codes.numel() == self.lib.skim_group_code_words(n, m) and scales.numel() == self.lib.skim_group_scale_entries(n, m, group)
+        assert codes.device == scales.device == self.device and group in (32, 64, 128)
+        blocks = -(-n // 16) * -(-m // 128)
+        assert codes.numel() == 256 * blocks and scales.numel() == 2048 // group * blocks, "codes and scales do not have the sizes of n, m, group"
         return codes.data_ptr(), scales.data_ptr(), n, m, group
 
     def _group_input(self, x, x_scales, m, what):
@@ -473,9 +473,9 @@ class Context:
         assert x_scales.numel() == T, what
         return p, E4M3, ld, x_scales.data_ptr(), T
 
-    def _group_scratch(self, n, m, T):
+    def _group_scratch(self, n, m, T, to_input):
         """(pointer, bytes, tensor) of the scratch of a product: it goes back to the allocator with this stream's work queued ahead of its next use."""
-        need = self.lib.skim_group_scratch_bytes(self.h, n, m, T)
+        need = self.lib.skim_group_scratch_bytes(self.h, n, m, T, to_input)
         if need == 0:
             return None, 0, None
         scratch = self.empty((need,), self.torch.uint8)
@@ -514,7 +514,7 @@ class Context:
         xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_matmul: x")
         dtype, yt = self._result_type(out, out_dtype)
         y = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_matmul: out")
-        sp, sb, _keep = self._group_scratch(n, m, T)
+        sp, sb, _keep = self._group_scratch(n, m, T, 0)
         self._check(self.lib.skim_group_matmul(self.h, codes, scales, n, m, group, xp, xt, ldx, xs, T, y.data_ptr(), yt, sp, sb))
         return y
 
@@ -524,7 +524,7 @@ class Context:
         dyp, ld, T = self._rows(dy, (self.torch.bfloat16,), n, "group_matmul_dx: dy")
         dtype, yt = self._result_type(out, out_dtype)
         dx = self._result(out, (m,) if dy.dim() == 1 else (T, m), dtype, "group_matmul_dx: out")
-        sp, sb, _keep = self._group_scratch(n, m, T)
+        sp, sb, _keep = self._group_scratch(n, m, T, 1)
         self._check(self.lib.skim_group_matmul_dx(self.h, codes, scales, n, m, group, dyp, ld, T, dx.data_ptr(), yt, sp, sb))
         return dx
 
@@ -536,7 +536,7 @@ class Context:
         xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_glu: x")
         dtype, yt = self._result_type(out, out_dtype)
         a = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_glu: out")
-        sp, sb, _keep = self._group_scratch(n, m, T)
+        sp, sb, _keep = self._group_scratch(n, m, T, 0)
         self._check(self.lib.skim_group_glu(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, a.data_ptr(), yt, sp, sb))
         return a
 
@@ -555,7 +555,7 @@ class Context:
         dgate = self._result(out.get("dgate"), lead + (n,), t.bfloat16, "group_glu_backward: dgate")
         dup = self._result(out.get("dup"), lead + (n,), t.bfloat16, "group_glu_backward: dup")
         dx = self._result(out.get("dx"), lead + (m,), t.bfloat16, "group_glu_backward: dx") if want_dx else None
-        sp, sb, _keep = self._group_scratch(n, m, T)
+        sp, sb, _keep = self._group_scratch(n, m, T, 2)
         self._check(self.lib.skim_group_glu_backward(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, dap, ldda, dgate.data_ptr(),
                                                      dup.data_ptr(), None if dx is None else dx.data_ptr(), BF16, sp, sb))
         return dict(dx=dx, dgate=dgate, dup=dup)

@@ -115,18 +115,19 @@ __device__ __forceinline__ gq_bf16x8 widen(gq_word2 v) {
 
 __device__ __forceinline__ gq_float4 mfma(gq_bf16x8 a, gq_bf16x8 b, gq_float4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// 8 values of a row of x from column col on as a matrix operand, zeros past column m.  VEC: rows start on borders of the octet's size and m is a
-// multiple of 8.
-template <int XT, bool VEC>
-__device__ __forceinline__ gq_bf16x8 load_x(const void *x, long long row0, long long col, long long m) {
-    typedef std::conditional_t<XT == SKIM_BF16, uint16_t, uint8_t> E;
-    typedef std::conditional_t<XT == SKIM_BF16, gq_word4, gq_word2> V;
-    const E *p = (const E *)x + row0 + col;
-    V v = {};
-    if constexpr (VEC) {
-        if (col < m) v = *(const V *)p;
-    } else {
-        if (col + 8 <= m) {
+// 8 values of a row of x, as they come from memory, from column col on; zeros past column m.  VEC: rows start on borders of the octet's size and m
+// is a multiple of 8.
+template <int XT>
+struct XOctet {
+    std::conditional_t<XT == SKIM_BF16, gq_word4, gq_word2> v;
+    template <bool VEC>
+    __device__ __forceinline__ void load(const void *x, long long row0, long long col, long long m) {
+        typedef std::conditional_t<XT == SKIM_BF16, uint16_t, uint8_t> E;
+        const E *p = (const E *)x + row0 + col;
+        if constexpr (VEC) {
+            if (col < m) v = *(const decltype(v) *)p;
+            else v = decltype(v){};
+        } else if (col + 8 <= m) {
             __builtin_memcpy(&v, p, sizeof(v));              // (one load, of any alignment)
         } else {
             E e[8];
@@ -135,62 +136,96 @@ __device__ __forceinline__ gq_bf16x8 load_x(const void *x, long long row0, long 
             __builtin_memcpy(&v, e, sizeof(v));
         }
     }
-    if constexpr (XT == SKIM_BF16) return __builtin_bit_cast(gq_bf16x8, v);
-    else return widen(v);
-}
+    __device__ __forceinline__ gq_bf16x8 operand() const {
+        if constexpr (XT == SKIM_BF16) return __builtin_bit_cast(gq_bf16x8, v);
+        else return widen(v);
+    }
+};
 
 // ---- few tokens ----------------------------------------------------------------------------------------------------------
 
-// A workgroup makes 16 rows of the result for 16 NT tokens; its wavefronts share the columns block by block, and their sums are added
-// up in LDS in the order of the wavefronts.
+// A workgroup makes 16 rows of the result for 16 tokens, or (NT = 2) 32 for 32; its wavefronts share the columns block by block, and their sums are added up in
+// LDS in the order of the wavefronts.  Codes enter the matrix cores as whole numbers; a group's sum is multiplied by the scale once.  Bound by
+// the codes' way from memory: a wavefront asks for U blocks at once, with their scales and their columns of x, before it takes the first apart.
 template <int XT, int NT, int G, int MODE, bool VEC>
-__global__ void __launch_bounds__(1024) group_few_kernel(MmArgs A, int chunks) {
-    constexpr int MATS = MODE == MM_PLAIN ? 1 : 2;
+__global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs A, int chunks) {
+    constexpr int RT = NT, MATS = MODE == MM_PLAIN ? 1 : 2, U = NT > 1 ? 1 : MATS * (GQ_COLS / G) * (XT == SKIM_BF16 ? 2 : 1) <= 2 ? 4 : 2, GS = GQ_COLS / G;
     extern __shared__ __align__(16) unsigned char few_lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nw = blockDim.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
     const int c = lane >> 4, l16 = lane & 15;
-    const long long rt = blockIdx.x / chunks, t0 = (long long)(blockIdx.x % chunks) * (16 * NT);
-    const long long kbs = gq_col_blocks(A.m), n16 = gq_row_blocks(A.n) * GQ_ROWS;
-    long long xrow[NT];
+    const long long rt0 = (long long)(blockIdx.x / chunks) * RT, t0 = (long long)(blockIdx.x % chunks) * (16 * NT);
+    const int kbs = (int)gq_col_blocks(A.m);
+    const long long rbs = gq_row_blocks(A.n), n16 = rbs * GQ_ROWS;
+    // (lanes without a token keep zeros and load nothing)
+    XOctet<XT> x[U][4][NT] = {};
+    gq_float4 acc[MATS][RT][NT] = {};
+    for (int first = wave; first < kbs; first += nw * U) {
+        gq_word4 w[U][MATS][RT];
+        gq_word2 s[U][MATS][RT][GS];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) xrow[j] = min(t0 + 16 * j + l16, A.T - 1) * A.ldx;
-    gq_float4 acc[MATS][NT] = {};
-    for (long long kb = wave; kb < kbs; kb += nw) {
-        gq_word4 w[MATS];
+        for (int u = 0; u < U; ++u) {
+            const int kb = first + u * nw;
+            if (kb >= kbs) continue;
 #pragma unroll
-        for (int a = 0; a < MATS; ++a) w[a] = A.codes[a][(rt * kbs + kb) * 64 + lane];
+            for (int a = 0; a < MATS; ++a)
 #pragma unroll
-        for (int g = 0; g < GQ_COLS / G; ++g) {
-            gq_float4 d[MATS][NT] = {};
+                for (int r = 0; r < RT; ++r) {
+                    const long long rt = min(rt0 + r, rbs - 1);
+                    w[u][a][r] = A.codes[a][(rt * kbs + kb) * 64 + lane];
 #pragma unroll
-            for (int k = g * (G / 32); k < (g + 1) * (G / 32); ++k) {
-                gq_bf16x8 b[NT];
+                    for (int g = 0; g < GS; ++g) s[u][a][r][g] = *(const gq_word2 *)(A.scales[a] + ((long long)kb * GS + g) * n16 + rt * GQ_ROWS + 4 * c);
+                }
 #pragma unroll
-                for (int j = 0; j < NT; ++j) b[j] = load_x<XT, VEC>(A.x, xrow[j], kb * GQ_COLS + 32 * k + 8 * c, A.m);
+            for (int j = 0; j < NT; ++j) {
+                const long long t = t0 + 16 * j + l16;
+                if (t < A.T) {
 #pragma unroll
-                for (int a = 0; a < MATS; ++a) {
-                    const gq_bf16x8 q = code_operand(w[a][k]);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) d[a][j] = mfma(q, b[j], d[a][j]);
+                    for (int k = 0; k < 4; ++k) x[u][k][j].template load<VEC>(A.x, t * A.ldx, (long long)kb * GQ_COLS + 32 * k + 8 * c, A.m);
                 }
             }
+        }
 #pragma unroll
-            for (int a = 0; a < MATS; ++a) {
-                const gq_word2 s = *(const gq_word2 *)(A.scales[a] + (kb * (GQ_COLS / G) + g) * n16 + rt * GQ_ROWS + 4 * c);
-                const gq_float4 f{gq_scale(s[0] & 0xFFFF), __uint_as_float(s[0] & 0xFFFF0000u), gq_scale(s[1] & 0xFFFF), __uint_as_float(s[1] & 0xFFFF0000u)};
+        for (int u = 0; u < U; ++u) {
+            if (first + u * nw >= kbs) continue;
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+            for (int g = 0; g < GS; ++g) {
+                gq_float4 d[MATS][RT][NT] = {};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[a][j][i] = fmaf(f[i], d[a][j][i], acc[a][j][i]);
+                for (int k = g * (4 / GS); k < (g + 1) * (4 / GS); ++k) {
+                    gq_bf16x8 b[NT];
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) b[j] = x[u][k][j].operand();
+#pragma unroll
+                    for (int a = 0; a < MATS; ++a)
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) {
+                            const gq_bf16x8 q = code_operand(w[u][a][r][k]);
+#pragma unroll
+                            for (int j = 0; j < NT; ++j) d[a][r][j] = mfma(q, b[j], d[a][r][j]);
+                        }
+                }
+#pragma unroll
+                for (int a = 0; a < MATS; ++a)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        const gq_word2 v = s[u][a][r][g];
+                        const gq_float4 f{gq_scale(v[0] & 0xFFFF), __uint_as_float(v[0] & 0xFFFF0000u), gq_scale(v[1] & 0xFFFF), __uint_as_float(v[1] & 0xFFFF0000u)};
+#pragma unroll
+                        for (int j = 0; j < NT; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[a][r][j][i] = fmaf(f[i], d[a][r][j][i], acc[a][r][j][i]);
+                    }
             }
         }
     }
-    constexpr int E = NT * 64;           // fours of a wavefront's sums, for one matrix
+    constexpr int E = RT * NT * 64;      // fours of a wavefront's sums, for one matrix
     gq_float4 *red = (gq_float4 *)few_lds;
 #pragma unroll
     for (int a = 0; a < MATS; ++a)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) red[((wave * MATS + a) * NT + j) * 64 + lane] = acc[a][j];
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) red[(wave * MATS + a) * E + (r * NT + j) * 64 + lane] = acc[a][r][j];
     __syncthreads();
     for (int e = tid; e < E; e += blockDim.x) {
         gq_float4 v[MATS] = {};
@@ -198,7 +233,7 @@ __global__ void __launch_bounds__(1024) group_few_kernel(MmArgs A, int chunks) {
         for (int a = 0; a < MATS; ++a)
             for (int w = 0; w < nw; ++w) v[a] += red[(w * MATS + a) * E + e];
         const int el = e & 63;
-        const long long t = t0 + 16 * (e >> 6) + (el & 15);
+        const long long t = t0 + 16 * ((e >> 6) % NT) + (el & 15), rt = rt0 + (e >> 6) / NT;
         if (t < A.T) finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
     }
 }
@@ -212,9 +247,9 @@ __global__ void __launch_bounds__(1024) group_few_kernel(MmArgs A, int chunks) {
 // memory: codes come into registers a block ahead, one 16-byte load for 32 of them, and are taken apart there, times their scale, into
 // operands.  For dx, where a lane needs 8 rows of one column, they pass through 4 KB of LDS of the wavefront's own and come back by the transposing read.
 // LDS rows of a token are 256 bytes; its 16-byte unit u is at place u ^ (token % 16), so that 16 tokens' units of one column octet lie in different banks.
-constexpr int WIDE_TOKENS = 128, WIDE_R = 4, WIDE_THREADS = 64 * WIDE_R;
-constexpr int WIDE_X_BYTES = WIDE_TOKENS * GQ_COLS * 2;              // of one block: 32 KB
-constexpr int WIDE_A_BYTES = 2 * 16 * 64 * 2;                        // dx: a wavefront's 16 rows x 64 columns, twice
+constexpr int WIDE_R = 4, WIDE_THREADS = 64 * WIDE_R;
+constexpr int wide_x_bytes(int tt) { return 32 * tt * GQ_COLS * 2; }     // of one block: 32 KB for 128 tokens
+constexpr int WIDE_A_ROW = 144, WIDE_A_BYTES = 16 * WIDE_A_ROW;      // dx: a wavefront's 16 rows x 64 columns; rows 16 bytes further apart than they are long, for the banks
 
 // Scaled weights of a word, exact in bfloat16.
 __device__ __forceinline__ gq_word4 weight_operand(uint32_t w, float s) {
@@ -244,14 +279,18 @@ __device__ __forceinline__ void wide_finish(const MmArgs &A, long long w, long l
 
 // Four wavefronts side by side; with KS = 2 four more sum the other half of the columns, and the halves meet in LDS at the end.  `parts`
 // workgroups share a tile's columns further: their sums go to `partial`, and group_join_kernel adds them up.
-template <bool DX, int MODE, int KS>
+template <bool DX, int MODE, int KS, int TT>
 __global__ void __launch_bounds__(WIDE_THREADS *KS) __attribute__((amdgpu_waves_per_eu(2, 2)))
-group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int parts, gq_float4 *partial) {
+group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int whole, int rest, int rest_parts, gq_float4 *partial) {
     extern __shared__ __align__(16) unsigned char smem[];
+    constexpr int TOKENS = 32 * TT, X_BYTES = wide_x_bytes(TT);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane >> 4, l16 = lane & 15;
     const int kg = wave / WIDE_R, rg = wave % WIDE_R;
-    const int work = xcd_order(blockIdx.x, gridDim.x), part = work / tiles, tile = work - part * tiles;
-    const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * WIDE_TOKENS;
+    // the first `whole` workgroups take a tile each, the others a part of one of the `rest`
+    const bool shared = (int)blockIdx.x >= whole;
+    const int work = shared ? xcd_order(blockIdx.x - whole, gridDim.x - whole) : xcd_order(blockIdx.x, whole);
+    const int parts = shared ? rest_parts : 1, part = shared ? work / rest : 0, nth = work - part * rest, tile = shared ? whole + nth : work;
+    const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * TOKENS;
     const long long kbs = gq_col_blocks(A.m), rbs = gq_row_blocks(A.n), n16 = rbs * GQ_ROWS;
     const long long depth = DX ? A.n : A.m;                          // summed over
     const int blocks = (int)((depth + 127) / 128), total = DX ? blocks * mats : blocks;
@@ -260,10 +299,10 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
     const int kb0 = (int)((long long)total * share / shares), kb1 = (int)((long long)total * (share + 1) / shares);
     const int rounds = (total + shares - 1) / shares;                // (of the longest share: all wavefronts meet at every barrier)
 
-    // ---- the tokens' operand: 8 copies of 1 KB a wavefront and block, 4 tokens of 16 units each
-    unsigned char *const xbuf = smem + kg * 2 * WIDE_X_BYTES;
-    const uint32_t lds_x = (uint32_t)(uintptr_t)(lds_byte *)xbuf + (uint32_t)rg * 8192u;
-    const uint32_t ldb = (uint32_t)(A.ldx * 2), voff0 = (uint32_t)(rg * 32 + c) * ldb;       // of the token of copy 0
+    // ---- the tokens' operand: 2 TT copies of 1 KB a wavefront and block, 4 tokens of 16 units each
+    unsigned char *const xbuf = smem + kg * 2 * X_BYTES;
+    const uint32_t lds_x = (uint32_t)(uintptr_t)(lds_byte *)xbuf + (uint32_t)(rg * 2 * TT * 1024);
+    const uint32_t ldb = (uint32_t)(A.ldx * 2), voff0 = (uint32_t)(rg * 8 * TT + c) * ldb;       // of the token of copy 0
     const int unit0 = l16 ^ c;                                                               // its unit
     auto stage = [&](int kb, int place) {
         const int a = DX && kb >= blocks ? 1 : 0;
@@ -273,9 +312,9 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
         const LdsSource src{(uint64_t)(uintptr_t)((const uint16_t *)(a ? A.x2 : A.x) + t0 * A.ldx + col), ((A.T - 1 - t0) * A.ldx + (depth + 7) / 8 * 8 - col) * 2};
         const int4v rs = src.rsrc();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 2 * TT; ++i) {
             const int u = unit0 ^ 4 * (i & 3);
-            copy_to_lds(lds_x + place * WIDE_X_BYTES + i * 1024, u * 8 < left ? voff0 + (uint32_t)(4 * i) * ldb + (uint32_t)(u * 16) : 0x80000000u, rs);
+            copy_to_lds(lds_x + place * X_BYTES + i * 1024, u * 8 < left ? voff0 + (uint32_t)(4 * i) * ldb + (uint32_t)(u * 16) : 0x80000000u, rs);
         }
     };
 
@@ -336,22 +375,21 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
             }
         }
     };
-    unsigned char *mine = smem + 2 * KS * WIDE_X_BYTES + wave * WIDE_A_BYTES;
-    auto flip = [](int row) { return (2 * (row & 3)) ^ ((row >> 2) & 1); };    // dx: unit u of a row is at u ^ flip(row)
+    unsigned char *mine = smem + 2 * KS * X_BYTES + wave * WIDE_A_BYTES;
     auto operands = [&](int s, gq_bf16x8 (&a)[2]) {
         if constexpr (DX) {
             const uint32_t f = (uint32_t)__shfl((int)cscale[s >> 2], 16 * (s & 3) + l16, 64);
-            unsigned char *place = mine + (s & 1) * (WIDE_A_BYTES / 2);
+            // (one place for all half steps: a wavefront's accesses to LDS stay in their order)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                *(gq_word4 *)(place + l16 * 128 + ((4 * q + c) ^ flip(l16)) * 16) =
+                *(gq_word4 *)(mine + l16 * WIDE_A_ROW + c * 16 + q * 64) =
                     weight_operand(cur[s >> 1][2 * (s & 1) + q], q ? __uint_as_float(f & 0xFFFF0000u) : __uint_as_float(f << 16));
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 // 16 lanes read 4 rows of 16 columns and get 4 rows of one column each; a lane's operand: column lane % 32, rows 8 hi .. 8 hi + 7
-                const int row = 8 * hi + (l16 >> 2), u = 4 * i + 2 * (c & 1) + ((l16 & 3) >> 1);
-                const gq_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(place + row * 128 + (u ^ flip(row)) * 16 + (l16 & 1) * 8));
-                const gq_short4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(place + (row + 4) * 128 + (u ^ flip(row + 4)) * 16 + (l16 & 1) * 8));
+                const unsigned char *from = mine + (8 * hi + (l16 >> 2)) * WIDE_A_ROW + (c & 1) * 32 + (l16 & 3) * 8 + i * 64;
+                const gq_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)from);
+                const gq_short4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(from + 4 * WIDE_A_ROW));
                 a[i] = __builtin_bit_cast(gq_bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         } else {
@@ -366,10 +404,10 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
     // the next block's codes have come (and all copies with them)
     auto take_codes = [&]() {
         asm volatile("s_waitcnt vmcnt(0)"
-                     : "+v"(next[0]), "+v"(next[1]), "+v"(next[2]), "+v"(next[3]), "+v"(nscale[0]), "+v"(nscale[1]), "+v"(nscale[2]), "+v"(nscale[3]),
-                       "+v"(nscale[4]), "+v"(nscale[5]), "+v"(nscale[6]), "+v"(nscale[7])
+                     : "+v"(next[0]), "+v"(next[1]), "+v"(next[2]), "+v"(next[3]), "+v"(nscale[0]), "+v"(nscale[1]), "+v"(nscale[2]), "+v"(nscale[3])
                      :
                      : "memory");
+        if constexpr (!DX) asm volatile("" : "+v"(nscale[4]), "+v"(nscale[5]), "+v"(nscale[6]), "+v"(nscale[7]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) cur[i] = next[i];
         const uint32_t pick = lane & 1 ? 0x03020302u : 0x01000100u, both = lane & 1 ? 0x07060302u : 0x05040100u;       // the lane's row; of two registers
@@ -389,8 +427,8 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
         }
     };
 
-    floatx16 acc[2][4] = {};
-    gq_bf16x8 a[2][2], b[2][4];
+    floatx16 acc[2][TT] = {};
+    gq_bf16x8 a[2][2], b[2][TT];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         next[i] = gq_word4{};
@@ -411,11 +449,11 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
             stage(kb + 1, now ^ 1);
             load_codes(kb + 1);
         }
-        const unsigned char *xb = xbuf + now * WIDE_X_BYTES + (lane & 31) * (GQ_COLS * 2);
-        auto read_x = [&](int s, gq_bf16x8 (&v)[4]) {
+        const unsigned char *xb = xbuf + now * X_BYTES + (lane & 31) * (GQ_COLS * 2);
+        auto read_x = [&](int s, gq_bf16x8 (&v)[TT]) {
             const int place = (2 * s + hi) ^ l16;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(const gq_bf16x8 *)(xb + j * 32 * GQ_COLS * 2 + place * 16);
+            for (int j = 0; j < TT; ++j) v[j] = *(const gq_bf16x8 *)(xb + j * 32 * GQ_COLS * 2 + place * 16);
         };
         read_x(0, b[0]);
 #pragma unroll
@@ -428,47 +466,48 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
                 operands(0, a[0]);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < TT; ++j)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i], b[s & 1][j], acc[i][j], 0, 0, 0);
             if constexpr (!DX) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
+                for (int q = 0; q < 2 * TT; ++q) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    if (q < 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+                    if (q < TT) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 24 / TT, 0);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    int j0 = 0, j1 = 4;
+    int j0 = 0, j1 = TT;
     if constexpr (KS == 2) {                                         // each four give half of their sums and finish the others
-        floatx16 *give = (floatx16 *)smem + (size_t)wave * 256 + lane;
-        const floatx16 *take = (const floatx16 *)smem + (size_t)(wave ^ WIDE_R) * 256 + lane;
+        constexpr int H = TT / 2;
+        floatx16 *give = (floatx16 *)smem + (size_t)wave * (2 * H * 64) + lane;
+        const floatx16 *take = (const floatx16 *)smem + (size_t)(wave ^ WIDE_R) * (2 * H * 64) + lane;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) give[(i * 2 + j) * 64] = kg == 0 ? acc[i][j + 2] : acc[i][j];
+            for (int j = 0; j < H; ++j) give[(i * H + j) * 64] = kg == 0 ? acc[i][j + H] : acc[i][j];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const floatx16 o = take[(i * 2 + j) * 64];
+            for (int j = 0; j < H; ++j) {
+                const floatx16 o = take[(i * H + j) * 64];
                 if (kg == 0) acc[i][j] += o;
-                else acc[i][j + 2] += o;
+                else acc[i][j + H] += o;
             }
-        j0 = 2 * kg;
-        j1 = j0 + 2;
+        j0 = H * kg;
+        j1 = j0 + H;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (j < j0 || j >= j1) continue;
+    for (int j = 0; j < TT; ++j) {
+        if (j < j0 || j >= j1 || t0 + 32 * j >= A.T) continue;
         auto four = [&](int i, int q) { return gq_float4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}; };
         if (parts > 1) {
-            gq_float4 *p = partial + ((((size_t)part * tiles + tile) * WIDE_R + rg) * 4 + j) * 512 + lane;
+            gq_float4 *p = partial + ((((size_t)part * rest + nth) * WIDE_R + rg) * TT + j) * 512 + lane;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -481,13 +520,14 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tiles, int part
 }
 
 // The parts of a tile added up in their order, and finished: one wavefront for 32 tokens and 16 of a wavefront's rows.
-template <bool DX, int MODE>
-__global__ void __launch_bounds__(256) group_join_kernel(MmArgs A, int ttiles, int tiles, int parts, const gq_float4 *__restrict__ partial) {
+template <bool DX, int MODE, int TT>
+__global__ void __launch_bounds__(256) group_join_kernel(MmArgs A, int ttiles, int whole, int rest, int parts, const gq_float4 *__restrict__ partial) {
     const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const int tile = blockIdx.x / (4 * WIDE_R), rg = blockIdx.x / 4 % WIDE_R, j = blockIdx.x % 4;
-    const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * WIDE_TOKENS;
-    const gq_float4 *p = partial + (((size_t)tile * WIDE_R + rg) * 4 + j) * 512 + 2 * q * 64 + lane;
-    const size_t step = (size_t)tiles * WIDE_R * 4 * 512;
+    const int nth = blockIdx.x / (TT * WIDE_R), tile = whole + nth, rg = blockIdx.x / TT % WIDE_R, j = blockIdx.x % TT;
+    const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * (32 * TT);
+    if (t0 + 32 * j >= A.T) return;
+    const gq_float4 *p = partial + (((size_t)nth * WIDE_R + rg) * TT + j) * 512 + 2 * q * 64 + lane;
+    const size_t step = (size_t)rest * WIDE_R * TT * 512;
     gq_float4 v0 = p[0], v1 = p[64];
     for (int i = 1; i < parts; ++i) {
         v0 += p[i * step];
@@ -503,7 +543,9 @@ __global__ void __launch_bounds__(256) group_widen_kernel(const void *x, long lo
     const long long octets = columns / 8, at = (long long)blockIdx.x * 256 + threadIdx.x;
     if (at >= T * octets) return;
     const long long t = at / octets, col = (at - t * octets) * 8;
-    *(gq_bf16x8 *)(out + t * columns + col) = load_x<XT, false>(x, t * ldx, col, m);
+    XOctet<XT> v;
+    v.template load<false>(x, t * ldx, col, m);
+    *(gq_bf16x8 *)(out + t * columns + col) = v.operand();
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -515,8 +557,9 @@ void with_group(int group, F &&f) {
     else f(std::integral_constant<int, 128>{});
 }
 
-// From so many tokens on the tiles of 128 pay.
-constexpr int64_t WIDE_FROM = 65;
+// From so many tokens on the tiles pay.
+constexpr int64_t WIDE_FROM = 33;
+
 
 bool all_on(int64_t border, std::initializer_list<const void *> ps) {
     for (const void *p : ps)
@@ -524,19 +567,25 @@ bool all_on(int64_t border, std::initializer_list<const void *> ps) {
     return true;
 }
 
-// How the tiles of a product are shared out: `ks` times four wavefronts a workgroup, `parts` workgroups a tile.
+// How the tiles of a product are shared out: `ks` times four wavefronts a workgroup; `whole` workgroups with a tile each, `parts` for every one of
+// the `rest`.
 struct WidePlan {
-    int64_t ttiles, tiles;
-    int ks, parts;
-    size_t scratch() const { return parts > 1 ? (size_t)tiles * parts * WIDE_R * 4 * 512 * sizeof(gq_float4) : 0; }
+    int64_t ttiles, tiles, whole, rest;
+    int ks, parts, tt;
+    size_t scratch() const { return parts > 1 ? (size_t)rest * parts * WIDE_R * tt * 512 * sizeof(gq_float4) : 0; }
+    void join_none() { whole = tiles, rest = 0, parts = 1; }
 };
 WidePlan wide_plan(const skim_ctx *ctx, int64_t out, int64_t per, int64_t blocks, int64_t T) {
     WidePlan p;
-    p.ttiles = (T + WIDE_TOKENS - 1) / WIDE_TOKENS;
+    p.tt = T <= 64 ? 2 : 4;
+    p.ttiles = (T + 32 * p.tt - 1) / (32 * p.tt);
     p.tiles = (out + per - 1) / per * p.ttiles;
-    p.ks = p.tiles <= ctx->num_cu && blocks >= 4 ? 2 : 1;
-    p.parts = 1;
-    if (p.ks == 2) p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ctx->num_cu / p.tiles, blocks / 8));
+    p.join_none();
+    p.ks = 2 * p.tiles <= 3 * ctx->num_cu && blocks >= 4 ? 2 : 1;
+    if (p.ks == 2) {
+        const int64_t rest = p.tiles % ctx->num_cu, parts = rest ? std::min<int64_t>(ctx->num_cu / rest, blocks / 4) : 1;
+        if (parts > 1) p.whole = p.tiles - rest, p.rest = rest, p.parts = (int)parts;
+    }
     return p;
 }
 
@@ -578,24 +627,29 @@ skim_status launch_wide(skim_ctx *ctx, MmArgs A, int group, int x_type, int mats
         scratch_bytes -= need;
     }
     WidePlan p = wide_plan(ctx, DX ? A.m : A.n, MODE == MM_PLAIN ? 256 : 128, (depth + 127) / 128 * mats, A.T);
-    if (p.scratch() > scratch_bytes) p.parts = 1;
+    if (p.scratch() > scratch_bytes) p.join_none();
     if (p.tiles > 0x3fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens are too many for one call", A.T);
-    const size_t lds = p.ks * (2 * WIDE_X_BYTES + (DX ? 4 * WIDE_A_BYTES : 0));
-    auto go = [&](auto split) -> hipError_t {
+    const size_t lds = p.ks * (2 * wide_x_bytes(p.tt) + (DX ? 4 * WIDE_A_BYTES : 0));
+    auto go = [&](auto split, auto tokens) -> hipError_t {
         constexpr int KS = decltype(split)::value;
-        auto *k = &group_wide_kernel<DX, MODE, KS>;
+        auto *k = &group_wide_kernel<DX, MODE, KS, decltype(tokens)::value>;
         hipError_t e = hipSuccess;
         if (lds > 64 * 1024) e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e == hipSuccess)
-            hipLaunchKernelGGL(k, dim3((unsigned)(p.tiles * p.parts)), dim3(WIDE_THREADS * KS), lds, ctx->stream, A, group, mats, (int)p.ttiles, (int)p.tiles, p.parts,
-                               (gq_float4 *)room);
+            hipLaunchKernelGGL(k, dim3((unsigned)(p.whole + p.rest * p.parts)), dim3(WIDE_THREADS * KS), lds, ctx->stream, A, group, mats, (int)p.ttiles,
+                               (int)p.whole, (int)p.rest, p.parts, (gq_float4 *)room);
         return e;
     };
-    SKIM_HIP(ctx, p.ks == 1 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{}));
+    auto by_tokens = [&](auto split) { return p.tt == 2 ? go(split, std::integral_constant<int, 2>{}) : go(split, std::integral_constant<int, 4>{}); };
+    SKIM_HIP(ctx, p.ks == 1 ? by_tokens(std::integral_constant<int, 1>{}) : by_tokens(std::integral_constant<int, 2>{}));
     SKIM_HIP(ctx, hipGetLastError());
     if (p.parts > 1) {
-        hipLaunchKernelGGL((group_join_kernel<DX, MODE>), dim3((unsigned)(p.tiles * WIDE_R * 4)), dim3(256), 0, ctx->stream, A, (int)p.ttiles, (int)p.tiles, p.parts,
-                           (const gq_float4 *)room);
+        auto join = [&](auto tokens) {
+            hipLaunchKernelGGL((group_join_kernel<DX, MODE, decltype(tokens)::value>), dim3((unsigned)(p.rest * WIDE_R * p.tt)), dim3(256), 0, ctx->stream, A,
+                               (int)p.ttiles, (int)p.whole, (int)p.rest, p.parts, (const gq_float4 *)room);
+        };
+        if (p.tt == 2) join(std::integral_constant<int, 2>{});
+        else join(std::integral_constant<int, 4>{});
         SKIM_HIP(ctx, hipGetLastError());
     }
     return SKIM_OK;
@@ -606,23 +660,24 @@ skim_status launch_forward(skim_ctx *ctx, MmArgs A, int group, int x_type, void 
     A.quads = A.n % 4 == 0 && all_on(16, {A.y, A.dgate, A.dup}) && (!A.da || (A.ldda % 4 == 0 && all_on(8, {A.da})));
     constexpr int MATS = MODE == MM_PLAIN ? 1 : 2;
     if (A.T >= WIDE_FROM) return launch_wide<false, MODE>(ctx, A, group, x_type, 1, scratch, scratch_bytes);
-    const int nt = A.T <= 16 ? 1 : A.T <= 32 ? 2 : 4;
-    const int64_t chunks = (A.T + 16 * nt - 1) / (16 * nt), groups = gq_row_blocks(A.n) * chunks;
+    // 16 rows a workgroup, 32 where every row block reads more than 16 tokens; enough wavefronts for 16 a compute unit, no more than there are blocks
+    const int nt = A.T <= 16 ? 1 : 2, rt = nt;
+    const int64_t chunks = (A.T + 16 * nt - 1) / (16 * nt), groups = (gq_row_blocks(A.n) + rt - 1) / rt * chunks;
     if (groups > 0x7fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens on %lld rows are too many for one call", A.T, A.n);
     int nw = 4;
-    while (nw < 16 && groups * nw < 8ll * ctx->num_cu && nw < gq_col_blocks(A.m) && nw * MATS * nt * 2048 <= 65536) nw *= 2;
-    const size_t lds = (size_t)nw * MATS * nt * 1024;
+    while (nw < (nt == 1 ? 16 : 8) && groups * nw < 16ll * ctx->num_cu && nw < gq_col_blocks(A.m)) nw *= 2;
+    const size_t lds = (size_t)nw * MATS * rt * nt * 1024;
     const int64_t octet = x_type == SKIM_BF16 ? 16 : 8, es = x_type == SKIM_BF16 ? 2 : 1;
     const bool vec = A.m % 8 == 0 && (A.ldx * es) % octet == 0 && (uintptr_t)A.x % octet == 0;
     with_group(group, [&](auto g) {
         auto go = [&](auto xt, auto ntc, auto v) {
-            hipLaunchKernelGGL((group_few_kernel<decltype(xt)::value, decltype(ntc)::value, decltype(g)::value, MODE, decltype(v)::value>), dim3((unsigned)groups),
+            constexpr int NT = decltype(ntc)::value;
+            hipLaunchKernelGGL((group_few_kernel<decltype(xt)::value, NT, decltype(g)::value, MODE, decltype(v)::value>), dim3((unsigned)groups),
                                dim3(64 * nw), lds, ctx->stream, A, (int)chunks);
         };
         auto by_nt = [&](auto xt, auto v) {
             if (nt == 1) go(xt, std::integral_constant<int, 1>{}, v);
-            else if (nt == 2) go(xt, std::integral_constant<int, 2>{}, v);
-            else go(xt, std::integral_constant<int, 4>{}, v);
+            else go(xt, std::integral_constant<int, 2>{}, v);
         };
         auto by_vec = [&](auto xt) {
             if (vec) by_nt(xt, std::true_type{});
@@ -672,13 +727,16 @@ MmArgs matrix_args(const uint32_t *codes, const uint16_t *scales, const uint32_t
 
 }  // namespace
 
-extern "C" size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T) {
-    if (!ctx || n < 1 || n > SKIM_GROUP_MAX || m < 1 || m > SKIM_GROUP_MAX || T < 1 || T > 0x7fffffff) return 0;
+extern "C" size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients) {
+    if (!ctx || n < 1 || n > SKIM_GROUP_MAX || m < 1 || m > SKIM_GROUP_MAX || T < 1 || T > 0x7fffffff || gradients < 0 || gradients > 2) return 0;
     const int64_t over_m = (m + 127) / 128, over_n = (n + 127) / 128;
-    // forward: x in another type or alignment, and the partial sums; to the input: the same for two gradients whose rows are not multiples of 8
-    const size_t to_out = std::max(wide_plan(ctx, n, 256, over_m, T).scratch(), wide_plan(ctx, n, 128, over_m, T).scratch());
-    const size_t to_in = std::max(wide_plan(ctx, m, 256, over_n, T).scratch(), wide_plan(ctx, m, 256, 2 * over_n, T).scratch());
-    return std::max(T < WIDE_FROM ? (size_t)0 : widened_bytes(m, T) + to_out, (n % 8 ? 2 : 1) * widened_bytes(n, T) + to_in);
+    // forward: x in another type or alignment, and the partial sums
+    const size_t forward = T < WIDE_FROM ? 0
+                                         : widened_bytes(m, T) + std::max(wide_plan(ctx, n, 256, over_m, T).scratch(), wide_plan(ctx, n, 128, over_m, T).scratch());
+    if (gradients == 0) return forward;
+    // to the input: the same for one gradient of any alignment, or two whose rows may not be multiples of 8
+    if (gradients == 1) return widened_bytes(n, T) + wide_plan(ctx, m, 256, over_n, T).scratch();
+    return std::max(forward, (n % 8 ? 2 * widened_bytes(n, T) : 0) + wide_plan(ctx, m, 256, 2 * over_n, T).scratch());
 }
 
 extern "C" skim_status skim_group_matmul(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
