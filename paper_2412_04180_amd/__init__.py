@@ -215,12 +215,16 @@ class Context:
         return a.value, b.value
 
     def empty(self, shape, dtype):
-        t = self.torch
+        return self._empties((shape, dtype))[0]
+
+    def _empties(self, *wanted):
+        """New tensors of the given (shape, dtype)."""
+        t, device = self.torch, self.device
         # outputs belong to the stream the kernels run on; entering it takes longer than a short kernel, and is left out where it is current
-        if t._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
-            return t.empty(shape, dtype=dtype, device=self.device)
+        if t._C._cuda_getCurrentRawStream(device.index) == self._raw_stream:
+            return [t.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
         with t.cuda.stream(self.stream):
-            return t.empty(shape, dtype=dtype, device=self.device)
+            return [t.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
 
     # -- clustering -----------------------------------------------------------
     def error_table(self, W, S, alpha=None, bmin=1, bmax=4, iters=30, want_centroids=True, want_upper=True,
@@ -572,13 +576,20 @@ class Context:
             assert residual.dtype == x.dtype and residual.shape == x.shape, "rms_norm: residual"
             rp, ldr, _ = self._rows(residual, (x.dtype,), m, "rms_norm: residual")
         wp = self._norm_weight(weight, m)
-        out = out or {}
-        h = self._result(out.get("h"), x.shape, x.dtype, "rms_norm: h") if residual is not None else None
-        y = self._result(out.get("y"), x.shape, x.dtype, "rms_norm: y") if want_y else None
-        q = self._result(out.get("q"), x.shape, t.float8_e4m3fn, "rms_norm: q") if want_q else None
-        scales = self._result(out.get("scales"), (rows,), t.float32, "rms_norm: scales") if want_q else None
-        rstd = self._result(out.get("rstd"), (rows,), t.float32, "rms_norm: rstd")
-        self._check(self.lib.skim_rms_norm(self.h, xp, ldx, rp, ldr, BF16 if x.dtype == t.bfloat16 else F32, wp, eps, rows, m,
+        shape, dtype = x.shape, x.dtype
+        wanted = [("rstd", (rows,), t.float32)]
+        if residual is not None:
+            wanted.append(("h", shape, dtype))
+        if want_q:
+            wanted += [("q", shape, t.float8_e4m3fn), ("scales", (rows,), t.float32)]
+        if want_y:
+            wanted.append(("y", shape, dtype))
+        if out is None:
+            new = dict(zip((w[0] for w in wanted), self._empties(*[w[1:] for w in wanted])))
+        else:
+            new = {name: self._result(out.get(name), s, d, "rms_norm: " + name) for name, s, d in wanted}
+        h, q, scales, y, rstd = new.get("h"), new.get("q"), new.get("scales"), new.get("y"), new["rstd"]
+        self._check(self.lib.skim_rms_norm(self.h, xp, ldx, rp, ldr, BF16 if dtype == t.bfloat16 else F32, wp, eps, rows, m,
                                            None if h is None else h.data_ptr(), None if y is None else y.data_ptr(),
                                            None if q is None else q.data_ptr(), None if scales is None else scales.data_ptr(), rstd.data_ptr()))
         return dict(h=h, q=q, scales=scales, y=y, rstd=rstd)

@@ -1,15 +1,18 @@
 // Root-mean-square norm of a decoder block with the residual's addition and an 8-bit output, and its backward pass.
 #include "skim_common.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace {
 
 constexpr int NORM_OCTET = 8;          // neighbouring columns of a thread: 16 bytes of bfloat16
 constexpr int NORM_MAX_THREADS = 1024;
+constexpr int NORM_RESIDENT = 2048;   // threads of a compute unit
 constexpr double E4M3_MAX = 448.0;
 
 typedef float float8v __attribute__((ext_vector_type(8)));
+typedef float8v float8u __attribute__((aligned(16)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 
@@ -17,33 +20,45 @@ __device__ __forceinline__ float bf16_to_f32(uint32_t bits) { return __uint_as_f
 __device__ __forceinline__ uint32_t f32_to_bf16(float v) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v); }
 
 // Eight values of a row from column c on (zeros past column m).  VEC: the row starts on a 16-byte border and m is a
-// multiple of 8, so that an octet is whole or not there.
+// multiple of 8, so that an octet is whole or not there.  They stay as they came until they are asked for: what is done to a value waits for it.
+template <typename T, bool VEC>
+struct Octet {
+    std::conditional_t<VEC && sizeof(T) == 2, uint4v, float8v> v;
+    __device__ __forceinline__ void load(const T *row, int c, int m) {
+        v = decltype(v){};
+        if constexpr (VEC) {
+            if (c < m) {
+                if constexpr (sizeof(T) == 2) v = *(const uint4v *)(row + c);
+                else v = *(const float8u *)(row + c);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < m) {
+                    if constexpr (sizeof(T) == 2) v[i] = bf16_to_f32(row[c + i]);
+                    else v[i] = row[c + i];
+                }
+        }
+    }
+    __device__ __forceinline__ float8v get() const {
+        if constexpr (VEC && sizeof(T) == 2) {
+            float8v o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[2 * i] = __uint_as_float(v[i] << 16);
+                o[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+            }
+            return o;
+        } else {
+            return v;
+        }
+    }
+};
 template <typename T, bool VEC>
 __device__ __forceinline__ float8v load8(const T *row, int c, int m) {
-    float8v v = {};
-    if constexpr (VEC) {
-        if (c < m) {
-            if constexpr (sizeof(T) == 2) {
-                const uint4v u = *(const uint4v *)(row + c);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[2 * i] = __uint_as_float(u[i] << 16);
-                    v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-                }
-            } else {
-                const float4 a = *(const float4 *)(row + c), b = *(const float4 *)(row + c + 4);
-                v = float8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < m) {
-                if constexpr (sizeof(T) == 2) v[i] = bf16_to_f32(row[c + i]);
-                else v[i] = row[c + i];
-            }
-    }
-    return v;
+    Octet<T, VEC> o;
+    o.load(row, c, m);
+    return o.get();
 }
 
 template <typename T, bool VEC>
@@ -82,103 +97,134 @@ __device__ __forceinline__ float as_stored(float v) {
     return v;
 }
 
-// v (at most 448 in size) in float32 rounded to odd: what is rounded once more, to e4m3, then comes out as if it had been
-// rounded once.
-__device__ __forceinline__ float to_odd(double v) {
-    const float f = (float)v;
-    const double d = (double)f;
-    uint32_t u = __float_as_uint(f);
-    u -= fabs(d) > fabs(v) ? 1u : 0u;
-    u |= d != v ? 1u : 0u;
-    return __uint_as_float(u);
+// Eight values below 464 in size, ahead of their rounding to e4m3: in float32, on the same side of every number halfway between two of e4m3 as
+// the float64 value, and on none unless that is.  Those numbers have at most 5 significant bits; where the nearest float32 has no more and is not
+// the value, the one next to it towards the value is as good.  (One octet in 16000 of other values comes to that.)
+__device__ __forceinline__ void off_ties(const double (&v)[8], float (&o)[8]) {
+    bool few = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        o[i] = (float)v[i];
+        few |= (__float_as_uint(o[i]) & 0x7FFFF) == 0;
+    }
+    if (few) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t u = __float_as_uint(o[i]);
+            // (0: v is 0, or below the least float32 and rounds to 0)
+            if ((u & 0x7FFFF) == 0 && o[i] != 0.f && (double)o[i] != v[i]) o[i] = __uint_as_float(u + (fabs((double)o[i]) > fabs(v[i]) ? 0xFFFFFFFFu : 1u));
+        }
+    }
 }
 
 // h = x + residual (stored as x is), rstd = 1 / sqrt(mean h^2 + eps), y = h rstd weight, and y in e4m3 with one scale a row,
 // max |y| / 448.
-// Bound by memory: bfloat16 x, residual in, h and the 8-bit output out are 7 bytes a value.  One workgroup a row, the row in registers
-// (R octets a thread), both statistics in one reduction: max |h weight| does not need rstd.  They and the quotient that is rounded
+// Bound by memory: bfloat16 x, residual in, h and the 8-bit output out are 7 bytes a value.  A workgroup takes every so many rows, a row at a
+// time in registers (R octets a thread) with the weights beside it, and the next row on its way; both statistics in one reduction: max |h weight|
+// does not need rstd.  They and the quotient that is rounded
 // to 8 bits are float64: a code is then the one that the definition gives, also next to a border, and nobody can see in which
-// order the row was summed.  The float64 units do as many operations a clock as the float32 ones here, and about 20 a value are
-// half of what the memory takes.
+// order the row was summed.
 template <typename T, int R, bool VEC>
 __global__ void __launch_bounds__(NORM_MAX_THREADS)
-rms_norm_kernel(const T *x, long long ldx, const T *residual, long long ldr, const float *__restrict__ weight, float eps,
+rms_norm_kernel(const T *x, long long ldx, const T *residual, long long ldr, const float *__restrict__ weight, float eps, long long rows,
                 int m, T *h, T *y, uint8_t *q, float *scales, float *rstd_out) {
-    __shared__ double red[2][NORM_MAX_THREADS / 64];
-    const long long t = blockIdx.x;
+    __shared__ double red[2][2][NORM_MAX_THREADS / 64];
     const int tid = threadIdx.x, nth = blockDim.x;
+    constexpr bool KEEP = R <= 2, KEEP_P = R == 1, AHEAD = R <= 2;   // weights, products and the next row in registers, where there is room
+    const float8v ones{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    auto load_weight = [&](int r) { return weight ? load8<float, VEC>(weight, (r * nth + tid) * NORM_OCTET, m) : ones; };
     float8v v[R], w[R];
-    double sum = 0.0, top = 0.0;
+    double p[KEEP_P ? R : 1][8];
+    if (KEEP) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int c = (r * nth + tid) * NORM_OCTET;
-        v[r] = load8<T, VEC>(x + t * ldx, c, m);
-        if (weight) w[r] = load8<float, VEC>(weight, c, m);
-        else w[r] = float8v{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-        if (residual) {
-            const float8v e = load8<T, VEC>(residual + t * ldr, c, m);
+        for (int r = 0; r < R; ++r) w[r] = load_weight(r);
+    }
+    Octet<T, VEC> xr[R], er[R];
+    auto load_row = [&](long long t) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[r][i] = as_stored<T>(v[r][i] + e[i]);
-            store8<T, VEC>(h + t * m, c, m, v[r]);
+        for (int r = 0; r < R; ++r) {
+            const int c = (r * nth + tid) * NORM_OCTET;
+            xr[r].load(x + t * ldx, c, m);
+            if (residual) er[r].load(residual + t * ldr, c, m);
         }
+    };
+    if (AHEAD) load_row(blockIdx.x);
+    int turn = 0;
+    for (long long t = blockIdx.x; t < rows; t += gridDim.x, turn ^= 1) {
+        double sum = 0.0, top = 0.0;
+        if (!AHEAD) load_row(t);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double d = (double)v[r][i];
-            sum = fma(d, d, sum);
-            top = fmax(top, fabs(d * (double)w[r][i]));
-        }
-    }
+        for (int r = 0; r < R; ++r) {
+            const int c = (r * nth + tid) * NORM_OCTET;
+            v[r] = xr[r].get();
+            if (!KEEP) w[r] = load_weight(r);
+            if (residual) {
+                const float8v e = er[r].get();
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        sum += __shfl_xor(sum, d, 64);
-        top = fmax(top, __shfl_xor(top, d, 64));
-    }
-    if ((tid & 63) == 0) {
-        red[0][tid >> 6] = sum;
-        red[1][tid >> 6] = top;
-    }
-    __syncthreads();
-    sum = top = 0.0;
-    for (int i = 0; i < nth / 64; ++i) {
-        sum += red[0][i];
-        top = fmax(top, red[1][i]);
-    }
-    const double rstd = 1.0 / sqrt(sum / (double)m + (double)eps);
-    // (a scale below the least normal number would have digits missing; one row of zeros has none: 1)
-    const float scale = top > 0.0 ? fmaxf((float)(top * rstd / E4M3_MAX), 1.17549435e-38f) : 1.f;
-    if (tid == 0) {
-        if (rstd_out) rstd_out[t] = (float)rstd;
-        if (q) scales[t] = scale;
-    }
-    const double k = rstd / (double)scale;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int c = (r * nth + tid) * NORM_OCTET;
-        if (c >= m) continue;
-        if (y) {
-            float8v o;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = (float)((double)v[r][i] * (double)w[r][i] * rstd);
-            store8<T, VEC>(y + t * m, c, m, o);
-        }
-        if (q) {
-            float o[8];
+                for (int i = 0; i < 8; ++i) v[r][i] = as_stored<T>(v[r][i] + e[i]);
+                store8<T, VEC>(h + t * m, c, m, v[r]);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double e = (double)v[r][i] * (double)w[r][i] * k;
-                o[i] = to_odd(fmin(fmax(e, -E4M3_MAX), E4M3_MAX));
+                const double d = (double)v[r][i], e = d * (double)w[r][i];
+                sum = fma(d, d, sum);
+                top = fmax(top, fabs(e));
+                if (KEEP_P) p[r][i] = e;
             }
-            int lo = __builtin_amdgcn_cvt_pk_fp8_f32(o[0], o[1], 0, false);
-            lo = __builtin_amdgcn_cvt_pk_fp8_f32(o[2], o[3], lo, true);
-            int hi = __builtin_amdgcn_cvt_pk_fp8_f32(o[4], o[5], 0, false);
-            hi = __builtin_amdgcn_cvt_pk_fp8_f32(o[6], o[7], hi, true);
-            uint8_t *p = q + t * m + c;
-            if constexpr (VEC) {
-                *(uint2v *)p = uint2v{(uint32_t)lo, (uint32_t)hi};
-            } else {
+        }
+        if (AHEAD && t + gridDim.x < rows) load_row(t + gridDim.x);
+        auto product = [&](int r, int i) { return KEEP_P ? p[r][i] : (double)v[r][i] * (double)w[r][i]; };
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i < m) p[i] = (uint8_t)((uint32_t)(i < 4 ? lo : hi) >> (8 * (i & 3)));
+        for (int d = 32; d >= 1; d >>= 1) {
+            sum += __shfl_xor(sum, d, 64);
+            top = fmax(top, __shfl_xor(top, d, 64));
+        }
+        if ((tid & 63) == 0) {                           // (two sets: a row's are read while the next row's are written)
+            red[turn][0][tid >> 6] = sum;
+            red[turn][1][tid >> 6] = top;
+        }
+        __syncthreads();
+        sum = top = 0.0;
+        for (int i = 0; i < nth / 64; ++i) {
+            sum += red[turn][0][i];
+            top = fmax(top, red[turn][1][i]);
+        }
+        const double rstd = 1.0 / sqrt(sum / (double)m + (double)eps);
+        // (a scale below the least normal number would have digits missing; one row of zeros has none: 1)
+        const float scale = top > 0.0 ? fmaxf((float)(top * rstd / E4M3_MAX), 1.17549435e-38f) : 1.f;
+        if (tid == 0) {
+            if (rstd_out) rstd_out[t] = (float)rstd;
+            if (q) scales[t] = scale;
+        }
+        const double k = rstd / (double)scale;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int c = (r * nth + tid) * NORM_OCTET;
+            if (c >= m) continue;
+            if (y) {
+                float8v o;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = (float)(product(r, i) * rstd);
+                store8<T, VEC>(y + t * m, c, m, o);
+            }
+            if (q) {
+                double e[8];
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = product(r, i) * k;               // (at most 448 (1 + 2^-23))
+                off_ties(e, o);
+                int lo = __builtin_amdgcn_cvt_pk_fp8_f32(o[0], o[1], 0, false);
+                lo = __builtin_amdgcn_cvt_pk_fp8_f32(o[2], o[3], lo, true);
+                int hi = __builtin_amdgcn_cvt_pk_fp8_f32(o[4], o[5], 0, false);
+                hi = __builtin_amdgcn_cvt_pk_fp8_f32(o[6], o[7], hi, true);
+                uint8_t *to = q + t * m + c;
+                if constexpr (VEC) {
+                    *(uint2v *)to = uint2v{(uint32_t)lo, (uint32_t)hi};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i < m) to[i] = (uint8_t)((uint32_t)(i < 4 ? lo : hi) >> (8 * (i & 3)));
+                }
             }
         }
     }
@@ -194,30 +240,50 @@ rms_norm_back_kernel(const T *__restrict__ dy, long long lddy, const T *__restri
     __shared__ float red[2][NORM_MAX_THREADS / 64];
     const int tid = threadIdx.x, nth = blockDim.x;
     const long long t0 = rows * blockIdx.x / gridDim.x, t1 = rows * (blockIdx.x + 1) / gridDim.x;
-    float8v w[R], dw[R];
+    constexpr bool KEEP = R <= 2;                        // the weights in registers, where there is room; and with one octet a thread the next row
+    const float8v ones{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    auto load_weight = [&](int r) { return weight ? load8<float, VEC>(weight, (r * nth + tid) * NORM_OCTET, m) : ones; };
+    float8v w[KEEP ? R : 1], dw[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         dw[r] = float8v{};
-        if (weight) w[r] = load8<float, VEC>(weight, (r * nth + tid) * NORM_OCTET, m);
-        else w[r] = float8v{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        if (KEEP) w[r] = load_weight(r);
     }
-    for (long long t = t0; t < t1; ++t) {
-        const float rs = rstd[t];
-        float8v g[R], n[R];
-        float sum = 0.f;
+    Octet<T, VEC> gr[R], nr[R], er[1];
+    float rs1 = 0.f;
+    auto load_row = [&](long long t) {
+        rs1 = rstd[t];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int c = (r * nth + tid) * NORM_OCTET;
-            g[r] = load8<T, VEC>(dy + t * lddy, c, m);
-            n[r] = load8<T, VEC>(h + t * ldh, c, m) * rs;
+            gr[r].load(dy + t * lddy, c, m);
+            nr[r].load(h + t * ldh, c, m);
+            if (R == 1 && dh) er[0].load(dh + t * lddh, c, m);
+        }
+    };
+    if (R == 1 && t0 < t1) load_row(t0);
+    for (long long t = t0; t < t1; ++t) {
+        if (R > 1) load_row(t);
+        float8v g[R], n[R], e = {};
+        const float rs = rs1;
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            g[r] = gr[r].get();
+            n[r] = nr[r].get() * rs;
+            const float8v wr = KEEP ? w[KEEP ? r : 0] : load_weight(r);
             float part = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 dw[r][i] = fmaf(g[r][i], n[r][i], dw[r][i]);
-                g[r][i] *= w[r][i];
+                g[r][i] *= wr[i];
                 part = fmaf(g[r][i], n[r][i], part);
             }
             sum += part;
+        }
+        if (R == 1) {
+            if (dh) e = er[0].get();
+            if (t + 1 < t1) load_row(t + 1);
         }
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
@@ -233,7 +299,7 @@ rms_norm_back_kernel(const T *__restrict__ dy, long long lddy, const T *__restri
             float8v o;
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = rs * fmaf(-n[r][i], mean, g[r][i]);
-            if (dh) o += load8<T, VEC>(dh + t * lddh, c, m);
+            if (dh) o += R == 1 ? e : load8<T, VEC>(dh + t * lddh, c, m);
             store8<T, VEC>(dx + t * m, c, m, o);
         }
     }
@@ -248,26 +314,32 @@ rms_norm_back_kernel(const T *__restrict__ dy, long long lddy, const T *__restri
     }
 }
 
-// dweight: the partial rows added up, 64 columns a workgroup, its wavefronts taking every 16th row.
-constexpr int NORM_COL_WAVES = 16;
-__global__ void __launch_bounds__(64 * NORM_COL_WAVES) norm_columns_kernel(const float *__restrict__ partial, int parts, int m, float *dweight) {
-    __shared__ float red[NORM_COL_WAVES][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+// dweight: the partial rows added up, 16 columns a workgroup, its 64 groups of lanes taking every 64th row.
+constexpr int NORM_COL_GROUPS = 64;
+__global__ void __launch_bounds__(16 * NORM_COL_GROUPS) norm_columns_kernel(const float *__restrict__ partial, int parts, int m, float *dweight) {
+    __shared__ float red[NORM_COL_GROUPS][17];
+    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
     float sum = 0.f;
     if (c < m)
-        for (int p = wave; p < parts; p += NORM_COL_WAVES) sum += partial[(long long)p * m + c];
-    red[wave][lane] = sum;
+        for (int p = group; p < parts; p += NORM_COL_GROUPS) sum += partial[(long long)p * m + c];
+    red[group][lane] = sum;
     __syncthreads();
-    if (wave == 0 && c < m) {
+    if (group < 16) {                                    // column `group`: 16 lanes add 4 each, then each other's
         sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < NORM_COL_WAVES; ++i) sum += red[i][lane];
-        dweight[c] = sum;
+        for (int i = 0; i < NORM_COL_GROUPS / 16; ++i) sum += red[lane + 16 * i][group];
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 16);
+        if (lane == 0 && blockIdx.x * 16 + group < m) dweight[blockIdx.x * 16 + group] = sum;
     }
 }
 
-// Octets a thread keeps of a row and threads a workgroup: one octet up to 8192 columns, then up to four.
+// Octets a thread keeps of a row: one up to 8192 columns, then up to four.  Forward, where there are rows for every compute unit, two from 512
+// columns on: the reductions, the root and the divisions cost a wavefront as much as an octet.  (float32 rows are bound by memory as they are.)
 int norm_octets(int64_t m) { return m <= 8192 ? 1 : m <= 16384 ? 2 : 4; }
+int norm_forward_octets(const skim_ctx *ctx, int type, int64_t rows, int64_t m) {
+    return type == SKIM_BF16 && m > 512 && m <= 8192 && rows >= 2 * ctx->num_cu ? 2 : norm_octets(m);
+}
 int norm_threads(int64_t m, int r) {
     const int64_t per = 64ll * NORM_OCTET * r;
     return (int)((m + per - 1) / per * 64);
@@ -281,9 +353,9 @@ int64_t norm_back_groups(const skim_ctx *ctx, int64_t rows, int64_t m) {
 }
 
 template <typename F>
-void with_shape(int64_t m, bool vec, F &&f) {
+void with_shape(int octets, bool vec, F &&f) {
     auto pick = [&](auto v) {
-        switch (norm_octets(m)) {
+        switch (octets) {
             case 1: f(std::integral_constant<int, 1>{}, v); break;
             case 2: f(std::integral_constant<int, 2>{}, v); break;
             default: f(std::integral_constant<int, 4>{}, v); break;
@@ -321,10 +393,12 @@ extern "C" skim_status skim_rms_norm(skim_ctx *ctx, const void *x, int64_t ldx, 
                      ((uintptr_t)q_e4m3 & 7) == 0;
     auto launch = [&](auto zero) {
         using T = decltype(zero);
-        with_shape(m, vec, [&](auto r, auto v) {
+        with_shape(norm_forward_octets(ctx, type, rows, m), vec, [&](auto r, auto v) {
             constexpr int R = decltype(r)::value;
-            hipLaunchKernelGGL((rms_norm_kernel<T, R, decltype(v)::value>), dim3((unsigned)rows), dim3(norm_threads(m, R)), 0, ctx->stream, (const T *)x,
-                               (long long)ldx, (const T *)residual, (long long)ldr, weight, eps, (int)m, (T *)h, (T *)y, q_e4m3, scales, rstd);
+            const int nth = norm_threads(m, R);
+            const int64_t groups = std::min<int64_t>(rows, (int64_t)ctx->num_cu * NORM_RESIDENT / nth);
+            hipLaunchKernelGGL((rms_norm_kernel<T, R, decltype(v)::value>), dim3((unsigned)groups), dim3(nth), 0, ctx->stream, (const T *)x, (long long)ldx,
+                               (const T *)residual, (long long)ldr, weight, eps, (long long)rows, (int)m, (T *)h, (T *)y, q_e4m3, scales, rstd);
         });
     };
     if (type == SKIM_BF16) launch((uint16_t)0);
@@ -358,7 +432,7 @@ extern "C" skim_status skim_rms_norm_backward(skim_ctx *ctx, const void *dy, int
     float *partial = dweight ? (float *)scratch : nullptr;
     auto launch = [&](auto zero) {
         using T = decltype(zero);
-        with_shape(m, vec, [&](auto r, auto v) {
+        with_shape(norm_octets(m), vec, [&](auto r, auto v) {
             constexpr int R = decltype(r)::value;
             hipLaunchKernelGGL((rms_norm_back_kernel<T, R, decltype(v)::value>), dim3((unsigned)groups), dim3(norm_threads(m, R)), 0, ctx->stream,
                                (const T *)dy, (long long)lddy, (const T *)h, (long long)ldh, (const T *)dh, (long long)lddh, rstd, weight, (long long)rows,
@@ -371,7 +445,7 @@ extern "C" skim_status skim_rms_norm_backward(skim_ctx *ctx, const void *dy, int
         SKIM_HIP(ctx, hipGetLastError());
     }
     if (dweight) {                                       // (no rows: zeros)
-        hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)((m + 63) / 64)), dim3(64 * NORM_COL_WAVES), 0, ctx->stream, partial, (int)groups, (int)m,
+        hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)((m + 15) / 16)), dim3(16 * NORM_COL_GROUPS), 0, ctx->stream, partial, (int)groups, (int)m,
                            dweight);
         SKIM_HIP(ctx, hipGetLastError());
     }
