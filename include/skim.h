@@ -319,7 +319,7 @@ skim_status skim_group_unpack(skim_ctx *ctx, const uint32_t *codes, const uint16
  * Operands are exact and sums float32; a result is rounded once, to its type.  What x holds behind a row's m columns is not used.
  * scratch (dev, 16-byte aligned; NULL with 0 bytes = none): skim_group_scratch_bytes(ctx, n, m, T, gradients) bytes, gradients = 0 for
  * skim_group_matmul and skim_group_glu, 1 for skim_group_matmul_dx, 2 for skim_group_glu_backward (n x m: the matrices; 0 for arguments that
- * the calls reject, and for few tokens forward).  It takes x in bfloat16 where rows come in e4m3 or off the 16-byte borders, without room for which
+ * the calls reject, and for up to 64 tokens forward).  It takes x in bfloat16 where rows come in e4m3 or off the 16-byte borders, without room for which
  * calls on more than 64 tokens and gradients are refused (SKIM_ERR_WORKSPACE); and partial sums, up to 32 MB, where the results have few tiles and
  * several compute units share one: without room for them the call is slower.  The order of the sums, and so their last digits, depend on
  * that. */

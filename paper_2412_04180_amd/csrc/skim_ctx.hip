@@ -62,6 +62,7 @@ extern "C" skim_status skim_create(skim_ctx **out, int device, void *hip_stream)
     c->greedy_lds_enabled = 0;
     c->xtx_lds_enabled = 0;
     c->gemm3_lds_enabled = 0;
+    c->wide_lds_enabled = 0;
     c->validate = 0;
     c->pack_scratch = nullptr;
     c->sort_counters = nullptr;

@@ -240,13 +240,18 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
 
 // ---- many tokens -----------------------------------------------------------------------------------------------------------
 
-// y = x W^T, the gated block and its backward pass, and dx = dy W (+ dy2 W2), on tiles of the matrix cores.  A workgroup of four wavefronts makes
-// 256 rows of W (128 of gate and the same of up; for dx 256 columns) for 128 tokens, a wavefront 64 of them: 4 x 8 accumulator
-// tiles of 16 x 16.
-// The tokens' operand: 128 columns of x (rows of dy's matrix for dx) go to LDS a block ahead, in bfloat16.  The weights' operand never is in
+// y = x W^T, the gated block and its backward pass, and dx = dy W (+ dy2 W2), on tiles of the matrix cores.  Four wavefronts side by side make
+// 256 rows of W (128 of gate and the same of up; for dx 256 columns) for 128 tokens, each 64 of them: 2 x 4 accumulator
+// tiles of 32 x 32.
+// The tokens' operand: 128 columns of x (for dx as many values of dy) go straight to LDS a block ahead.  The weights' operand never is in
 // memory: codes come into registers a block ahead, one 16-byte load for 32 of them, and are taken apart there, times their scale, into
-// operands.  For dx, where a lane needs 8 rows of one column, they pass through 4 KB of LDS of the wavefront's own and come back by the transposing read.
+// operands, those of the next 16 columns between the matrix instructions of these (19 operations for 8 weights).  For dx, where a lane
+// needs 8 rows of one column, they pass through LDS of the wavefront's own and come back by the transposing read.
 // LDS rows of a token are 256 bytes; its 16-byte unit u is at place u ^ (token % 16), so that 16 tokens' units of one column octet lie in different banks.
+// 32 x 32 instructions: half as many as of 16 x 16 for the same product.  No wait stands between a load and the end of its block: a value that is
+// shifted or combined as it arrives is waited for at once, which cost 20 % when it happened to the scales.
+// Bound by the matrix cores and the power they draw: 2048 tokens on 8192 x 11008 run at 1.10-1.22 PFLOP/s (matrix products of bfloat16 matrices at
+// 1.45-1.5), on x of zeros at 1.46, without the taking apart at 1.33; two wavefronts a SIMD, 256 registers each, leave no room for tiles that would share it more.
 constexpr int WIDE_R = 4, WIDE_THREADS = 64 * WIDE_R;
 constexpr int wide_x_bytes(int tt) { return 32 * tt * GQ_COLS * 2; }     // of one block: 32 KB for 128 tokens
 constexpr int WIDE_A_ROW = 144, WIDE_A_BYTES = 16 * WIDE_A_ROW;      // dx: a wavefront's 16 rows x 64 columns; rows 16 bytes further apart than they are long, for the banks
@@ -537,7 +542,7 @@ __global__ void __launch_bounds__(256) group_join_kernel(MmArgs A, int ttiles, i
 }
 
 // x as the tiles take it: bfloat16, rows of `columns` values on 16-byte borders.  (In the tiles themselves the conversion of e4m3 through registers
-// cost 40 % of their time, for want of registers; this pass, bound by the 3 bytes a value, costs 4 % of it.)
+// cost 40 % of their time, for want of registers; this pass, bound by the 3 bytes a value, costs 3 % of it on 512 tokens of 4096 values.)
 template <int XT>
 __global__ void __launch_bounds__(256) group_widen_kernel(const void *x, long long ldx, long long T, int m, int columns, uint16_t *out) {
     const long long octets = columns / 8, at = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -557,8 +562,9 @@ void with_group(int group, F &&f) {
     else f(std::integral_constant<int, 128>{});
 }
 
-// From so many tokens on the tiles pay.
-constexpr int64_t WIDE_FROM = 33;
+// Forward, tiles from so many tokens on.  us on up to 64 tokens, few / tiles: 4096 x 4096 16 tokens 9.1 / 15.7, 64 11.4 / 17.8; 4096 x 11008 16 14.8 /
+// 21.5, 64 25.4 / 24.3; gated 11008 x 4096 16 18 / 29, 64 36 / 32, from e4m3 34 / 34; beyond 64 each chunk of 32 tokens reads all codes once more.
+constexpr int64_t WIDE_FROM = 65;
 
 
 bool all_on(int64_t border, std::initializer_list<const void *> ps) {
@@ -575,6 +581,11 @@ struct WidePlan {
     size_t scratch() const { return parts > 1 ? (size_t)rest * parts * WIDE_R * tt * 512 * sizeof(gq_float4) : 0; }
     void join_none() { whole = tiles, rest = 0, parts = 1; }
 };
+// Eight wavefronts a workgroup, one workgroup a compute unit, up to one tile and a half for each; four, two workgroups, beyond.  us with four / eight:
+// 64 tiles (512 tokens on 4096 x 4096) 70 / 39, 256 (2048 on 4096 x 11008) 178 / 164, 344 (512 on gated 11008 x 4096) 105 / 103, 512 (2048 on 8192 x 11008)
+// 308 / 330.  With eight, the tiles beyond a whole number for every compute unit are cut along the sum into as many parts as there are units left for
+// each; a part is at least 4 blocks of 128.  Tiles of 64 tokens (gradients; forward there are always more) where there are no more: 64 on 4096 x 11008
+// 25 us, 29 with half-empty ones.
 WidePlan wide_plan(const skim_ctx *ctx, int64_t out, int64_t per, int64_t blocks, int64_t T) {
     WidePlan p;
     p.tt = T <= 64 ? 2 : 4;
@@ -634,13 +645,21 @@ skim_status launch_wide(skim_ctx *ctx, MmArgs A, int group, int x_type, int mats
         constexpr int KS = decltype(split)::value;
         auto *k = &group_wide_kernel<DX, MODE, KS, decltype(tokens)::value>;
         hipError_t e = hipSuccess;
-        if (lds > 64 * 1024) e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const unsigned bit = 1u << (DX ? 2 * (KS - 1) + (decltype(tokens)::value == 4) : 4 + MODE);      // (forward four wavefronts need no more than 64 KB)
+        if (lds > 64 * 1024 && !(ctx->wide_lds_enabled & bit)) {
+            e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e == hipSuccess) ctx->wide_lds_enabled |= bit;
+        }
         if (e == hipSuccess)
             hipLaunchKernelGGL(k, dim3((unsigned)(p.whole + p.rest * p.parts)), dim3(WIDE_THREADS * KS), lds, ctx->stream, A, group, mats, (int)p.ttiles,
                                (int)p.whole, (int)p.rest, p.parts, (gq_float4 *)room);
         return e;
     };
-    auto by_tokens = [&](auto split) { return p.tt == 2 ? go(split, std::integral_constant<int, 2>{}) : go(split, std::integral_constant<int, 4>{}); };
+    auto by_tokens = [&](auto split) {
+        if constexpr (DX)
+            if (p.tt == 2) return go(split, std::integral_constant<int, 2>{});
+        return go(split, std::integral_constant<int, 4>{});
+    };
     SKIM_HIP(ctx, p.ks == 1 ? by_tokens(std::integral_constant<int, 1>{}) : by_tokens(std::integral_constant<int, 2>{}));
     SKIM_HIP(ctx, hipGetLastError());
     if (p.parts > 1) {
@@ -648,8 +667,12 @@ skim_status launch_wide(skim_ctx *ctx, MmArgs A, int group, int x_type, int mats
             hipLaunchKernelGGL((group_join_kernel<DX, MODE, decltype(tokens)::value>), dim3((unsigned)(p.rest * WIDE_R * p.tt)), dim3(256), 0, ctx->stream, A,
                                (int)p.ttiles, (int)p.whole, (int)p.rest, p.parts, (const gq_float4 *)room);
         };
-        if (p.tt == 2) join(std::integral_constant<int, 2>{});
-        else join(std::integral_constant<int, 4>{});
+        if constexpr (DX) {
+            if (p.tt == 2) join(std::integral_constant<int, 2>{});
+            else join(std::integral_constant<int, 4>{});
+        } else {
+            join(std::integral_constant<int, 4>{});
+        }
         SKIM_HIP(ctx, hipGetLastError());
     }
     return SKIM_OK;
