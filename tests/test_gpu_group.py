@@ -360,7 +360,7 @@ def test_no_tokens_and_rows_behind_the_last(ctx):
 
 # ---- norm ---------------------------------------------------------------------------------------------------------------
 
-NORMS = [(1, 1), (1, 7), (3, 64), (5, 129), (2, 1000), (9, 4096), (4, 8200), (2, 11008), (2, 22016), (1, 32768), (600, 72)]
+NORMS = [(1, 1), (1, 7), (3, 64), (5, 129), (2, 1000), (9, 4096), (4, 8200), (2, 11008), (2, 22016), (1, 32768), (600, 72), (600, 1000), (1100, 5000)]
 
 
 def rows(rng, T, m, dtype, ld=None):
@@ -625,3 +625,140 @@ def test_refusals(ctx, gpu_lib):
         ctx.group_quantize(big, group=100)
     with pytest.raises(gpu_lib.SkimError):
         ctx.rms_norm(big, eps=0.0)
+
+
+# ---- how the work is shared out, memory far away, other streams -----------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,n,m", [(2048, 4352, 1030), (4096, 4352, 140), (512, 4096, 4096)])
+def test_many_tiles(ctx, T, n, m):
+    """272 tiles (256 whole ones, the rest in parts), 544 (four wavefronts a workgroup) and 64 (all in parts)."""
+    rng = np.random.default_rng(T + m)
+    gq, W = matrix(rng, n, m, 64)
+    x, s, value = inputs(rng, T, m, "e4m3")
+    want, size = value @ W.T, np.abs(value) @ np.abs(W).T
+    close(ctx.group_matmul(gq, x, x_scales=s, out_dtype=torch.float32), want, 2.0 ** -24 * np.abs(want) + loss(m) * size, "y")
+    if m < 1000:
+        return
+    tq, V = matrix(rng, m, n, 32)                              # (the other way round: a gradient with as many tiles)
+    dy, _, value = inputs(rng, T, m, "bf16")
+    want, size = value @ V, np.abs(value) @ np.abs(V)
+    close(ctx.group_matmul_dx(tq, dy, out_dtype=torch.float32), want, 2.0 ** -24 * np.abs(want) + loss(m) * size, "dx")
+
+
+@pytest.mark.gpu
+def test_without_scratch(ctx):
+    """Fewer workgroups share a tile then, with the same result to the last digits; what has to be converted first is refused."""
+    rng = np.random.default_rng(21)
+    T, n, m = 100, 300, 4096
+    gq, W = matrix(rng, n, m, 128)
+    x, _, value = inputs(rng, T, m, "bf16")
+    q, s, _ = inputs(rng, T, m, "e4m3")
+    lib, h = ctx.lib, ctx.h
+    y = torch.empty((T, n), device="cuda")
+    cp, sp = gq["codes"].data_ptr(), gq["scales"].data_ptr()
+    assert lib.skim_group_scratch_bytes(h, n, m, T, 0) > 0 and lib.skim_group_scratch_bytes(h, n, m, 64, 0) == 0
+    assert lib.skim_group_scratch_bytes(h, n, m, 0, 0) == lib.skim_group_scratch_bytes(h, n, m, T, 3) == 0
+    assert lib.skim_group_matmul(h, cp, sp, n, m, 128, x.data_ptr(), 1, m, None, T, y.data_ptr(), 0, None, 0) == 0
+    want, size = value @ W.T, np.abs(value) @ np.abs(W).T
+    close(y, want, 2.0 ** -24 * np.abs(want) + loss(m) * size, "y")
+    assert lib.skim_group_matmul(h, cp, sp, n, m, 128, q.data_ptr(), 2, m, s.data_ptr(), T, y.data_ptr(), 0, None, 0) == -4
+    assert b"scratch" in lib.skim_last_error(h)
+    dy, _, dvalue = inputs(rng, 5, n, "bf16")                 # rows of 300 values: not on 16-byte borders
+    dx = torch.empty((5, m), device="cuda")
+    assert lib.skim_group_matmul_dx(h, cp, sp, n, m, 128, dy.data_ptr(), n, 5, dx.data_ptr(), 0, None, 0) == -4
+    need = lib.skim_group_scratch_bytes(h, n, m, 5, 1)
+    scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+    assert lib.skim_group_matmul_dx(h, cp, sp, n, m, 128, dy.data_ptr(), n, 5, dx.data_ptr(), 0, scratch.data_ptr(), need) == 0
+    close(dx, dvalue @ W, 2.0 ** -24 * np.abs(dvalue @ W) + loss(n) * (np.abs(dvalue) @ np.abs(W)), "dx")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [40, 70])
+def test_rows_of_x_that_lie_far_apart(ctx, T):
+    """The last rows begin more than 2^31 values (4 GB) behind the first, further than a tile's copies reach."""
+    rng = np.random.default_rng(31)
+    n, m, ld = 64, 256, 1 << 26
+    gq, W = matrix(rng, n, m, 64)
+    v = torch.from_numpy(rng.standard_normal((T, m))).to(torch.bfloat16)
+    mem = torch.empty((T - 1) * ld + m, dtype=torch.bfloat16, device="cuda")
+    x = mem.as_strided((T, m), (ld, 1))
+    x.copy_(v.cuda())
+    want, size = v.double().numpy() @ W.T, np.abs(v.double().numpy()) @ np.abs(W).T
+    close(ctx.group_matmul(gq, x, out_dtype=torch.float32), want, 2.0 ** -24 * np.abs(want) + loss(m) * size, "y")
+    o = ctx.rms_norm(x, eps=1e-5, want_y=True)
+    h = v.double().numpy()
+    yv = h / np.sqrt((h * h).mean(1, keepdims=True) + float(np.float32(1e-5)))
+    close(o["y"], yv, U[torch.bfloat16] * 1.01 * np.abs(yv), "norm")
+    dy = mem.as_strided((T, n), (ld, 1))
+    d = v[:, :n].double().numpy()
+    close(ctx.group_matmul_dx(gq, dy, out_dtype=torch.float32), d @ W, 2.0 ** -24 * np.abs(d @ W) + loss(n) * (np.abs(d) @ np.abs(W)), "dx")
+    del mem, x, dy
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_matrices_of_more_than_2_31_bytes(ctx):
+    """The last 16 rows, 2.1 GB behind the first, against the same rows as a matrix of their own."""
+    n, m, G = (1 << 17) + 16, (1 << 15) + 128, 128
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    codes = torch.randint(-2 ** 31, 2 ** 31, ((n // 16) * (m // 128) * 256,), dtype=torch.int32, device="cuda", generator=gen)
+    scales = (torch.randint(16, 32, (m // G, n), device="cuda", generator=gen).float() / 1024).to(torch.bfloat16)
+    big = dict(codes=codes, scales=scales, n=n, m=m, group=G)
+    last = dict(codes=codes[-(m // 128) * 256:].clone(), scales=scales[:, -16:].contiguous(), n=16, m=m, group=G)
+    assert codes.numel() * 4 > 2 ** 31
+    D = ctx.group_unpack(last).cpu().double().numpy()
+    for T in (1, 40, 70):
+        x = torch.randn((T, m), device="cuda", generator=gen).to(torch.bfloat16)
+        v = x.cpu().double().numpy()
+        want, size = v @ D.T, np.abs(v) @ np.abs(D).T
+        y = ctx.group_matmul(big, x, out_dtype=torch.float32)
+        close(y[:, -16:], want, 2.0 ** -24 * np.abs(want) + loss(m) * size, f"T={T}")
+        del y
+        dy = torch.zeros((T, n), dtype=torch.bfloat16, device="cuda")
+        dy[:, -16:] = x[:, :16]
+        d = v[:, :16]
+        close(ctx.group_matmul_dx(big, dy, out_dtype=torch.float32), d @ D, 2.0 ** -24 * np.abs(d @ D) + loss(n) * (np.abs(d) @ np.abs(D)), f"dx T={T}")
+    del big, last, codes, scales
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_a_context_on_a_stream_that_is_not_current(gpu_lib, ctx):
+    """Its outputs and scratch belong to its stream, whatever is current where it is called."""
+    rng = np.random.default_rng(17)
+    gq, _ = matrix(rng, 300, 1000, 64)
+    x, s, _ = inputs(rng, 90, 1000, "e4m3")
+    ref = ctx.group_matmul(gq, x, x_scales=s)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    other = gpu_lib.Context(0, stream=stream)
+    try:
+        for _ in range(3):
+            y = other.group_matmul(gq, x, x_scales=s)
+            n = other.rms_norm(y, want_y=True)
+        stream.synchronize()
+        assert torch.equal(y, ref) and torch.equal(n["y"], ctx.rms_norm(ref, want_y=True)["y"])
+    finally:
+        other.close()
+
+
+@pytest.mark.gpu
+def test_infinities_and_nans_stay_in_their_token(ctx):
+    rng = np.random.default_rng(19)
+    for T in (3, 90):
+        gq, W = matrix(rng, 100, 300, 64)
+        x, _, value = inputs(rng, T, 300, "bf16")
+        want, size = value @ W.T, np.abs(value) @ np.abs(W).T
+        x[1, 7] = float("nan")
+        x[2, 299] = float("inf")
+        y = ctx.group_matmul(gq, x, out_dtype=torch.float32)
+        keep = [t for t in range(T) if t not in (1, 2)]
+        close(y[keep], want[keep], 2.0 ** -24 * np.abs(want[keep]) + loss(300) * size[keep], "others")
+        assert torch.isnan(y[1]).all() and not torch.isfinite(y[2]).all()
+        dy, _, dvalue = inputs(rng, T, 100, "bf16")
+        dy[1, 99] = float("nan")
+        dx = ctx.group_matmul_dx(gq, dy, out_dtype=torch.float32)
+        rest = [t for t in range(T) if t != 1]
+        close(dx[rest], (dvalue @ W)[rest], 2.0 ** -24 * np.abs(dvalue @ W)[rest] + loss(100) * (np.abs(dvalue) @ np.abs(W))[rest], "dx")
+        assert torch.isnan(dx[1]).all()
