@@ -474,15 +474,11 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int whole, int rest
             for (int j = 0; j < TT; ++j)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i], b[s & 1][j], acc[i][j], 0, 0, 0);
-            if constexpr (!DX) {
-#pragma unroll
-                for (int q = 0; q < 2 * TT; ++q) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    if (q < TT) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 24 / TT, 0);
-                }
-            }
             __builtin_amdgcn_sched_barrier(0);
+            // (a wavefront ahead of the other on its SIMD for every second half step: they take turns at the matrix cores and at taking codes apart; 315 ->
+            // 298 us where two workgroups share a compute unit)
+            if (s & 1) __builtin_amdgcn_s_setprio(0);
+            else __builtin_amdgcn_s_setprio(1);
         }
     }
     int j0 = 0, j1 = TT;
