@@ -458,6 +458,11 @@ class Context:
         assert tuple(out.shape) == tuple(shape) and out.dtype == dtype and out.device == self.device and out.is_contiguous(), what
         return out
 
+    def _results(self, wanted):
+        """Of every (out, shape, dtype, what): `out`, checked, or a new tensor."""
+        new = iter(self._empties(*[w[1:3] for w in wanted if w[0] is None]))
+        return iter([next(new) if w[0] is None else self._result(*w) for w in wanted])
+
     def _group_pointers(self, gq):
         codes, scales, n, m, group = gq["codes"], gq["scales"], gq["n"], gq["m"], gq["group"]
         assert codes.dtype == self.torch.int32 and scales.dtype == self.torch.bfloat16 and codes.is_contiguous() and scales.is_contiguous()
@@ -576,19 +581,20 @@ class Context:
             assert residual.dtype == x.dtype and residual.shape == x.shape, "rms_norm: residual"
             rp, ldr, _ = self._rows(residual, (x.dtype,), m, "rms_norm: residual")
         wp = self._norm_weight(weight, m)
-        shape, dtype = x.shape, x.dtype
-        wanted = [("rstd", (rows,), t.float32)]
+        shape, dtype, given = x.shape, x.dtype, out or {}
+        wanted = [(given.get("rstd"), (rows,), t.float32, "rms_norm: rstd")]
         if residual is not None:
-            wanted.append(("h", shape, dtype))
+            wanted.append((given.get("h"), shape, dtype, "rms_norm: h"))
         if want_q:
-            wanted += [("q", shape, t.float8_e4m3fn), ("scales", (rows,), t.float32)]
+            wanted.append((given.get("q"), shape, t.float8_e4m3fn, "rms_norm: q"))
+            wanted.append((given.get("scales"), (rows,), t.float32, "rms_norm: scales"))
         if want_y:
-            wanted.append(("y", shape, dtype))
-        if out is None:
-            new = dict(zip((w[0] for w in wanted), self._empties(*[w[1:] for w in wanted])))
-        else:
-            new = {name: self._result(out.get(name), s, d, "rms_norm: " + name) for name, s, d in wanted}
-        h, q, scales, y, rstd = new.get("h"), new.get("q"), new.get("scales"), new.get("y"), new["rstd"]
+            wanted.append((given.get("y"), shape, dtype, "rms_norm: y"))
+        new = self._results(wanted)
+        rstd = next(new)
+        h = next(new) if residual is not None else None
+        q, scales = (next(new), next(new)) if want_q else (None, None)
+        y = next(new) if want_y else None
         self._check(self.lib.skim_rms_norm(self.h, xp, ldx, rp, ldr, BF16 if dtype == t.bfloat16 else F32, wp, eps, rows, m,
                                            None if h is None else h.data_ptr(), None if y is None else y.data_ptr(),
                                            None if q is None else q.data_ptr(), None if scales is None else scales.data_ptr(), rstd.data_ptr()))

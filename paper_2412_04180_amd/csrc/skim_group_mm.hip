@@ -286,7 +286,7 @@ __device__ __forceinline__ void wide_finish(const MmArgs &A, long long w, long l
 // workgroups share a tile's columns further: their sums go to `partial`, and group_join_kernel adds them up.
 template <bool DX, int MODE, int KS, int TT>
 __global__ void __launch_bounds__(WIDE_THREADS *KS) __attribute__((amdgpu_waves_per_eu(2, 2)))
-group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int whole, int rest, int rest_parts, gq_float4 *partial) {
+group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int tile0, int whole, int rest, int rest_parts, gq_float4 *partial) {
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr int TOKENS = 32 * TT, X_BYTES = wide_x_bytes(TT);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane >> 4, l16 = lane & 15;
@@ -294,7 +294,7 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int whole, int rest
     // the first `whole` workgroups take a tile each, the others a part of one of the `rest`
     const bool shared = (int)blockIdx.x >= whole;
     const int work = shared ? xcd_order(blockIdx.x - whole, gridDim.x - whole) : xcd_order(blockIdx.x, whole);
-    const int parts = shared ? rest_parts : 1, part = shared ? work / rest : 0, nth = work - part * rest, tile = shared ? whole + nth : work;
+    const int parts = shared ? rest_parts : 1, part = shared ? work / rest : 0, nth = work - part * rest, tile = tile0 + (shared ? whole + nth : work);
     const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * TOKENS;
     const long long kbs = gq_col_blocks(A.m), rbs = gq_row_blocks(A.n), n16 = rbs * GQ_ROWS;
     const long long depth = DX ? A.n : A.m;                          // summed over
@@ -522,9 +522,9 @@ group_wide_kernel(MmArgs A, int group, int mats, int ttiles, int whole, int rest
 
 // The parts of a tile added up in their order, and finished: one wavefront for 32 tokens and 16 of a wavefront's rows.
 template <bool DX, int MODE, int TT>
-__global__ void __launch_bounds__(256) group_join_kernel(MmArgs A, int ttiles, int whole, int rest, int parts, const gq_float4 *__restrict__ partial) {
+__global__ void __launch_bounds__(256) group_join_kernel(MmArgs A, int ttiles, int first, int rest, int parts, const gq_float4 *__restrict__ partial) {
     const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const int nth = blockIdx.x / (TT * WIDE_R), tile = whole + nth, rg = blockIdx.x / TT % WIDE_R, j = blockIdx.x % TT;
+    const int nth = blockIdx.x / (TT * WIDE_R), tile = first + nth, rg = blockIdx.x / TT % WIDE_R, j = blockIdx.x % TT;
     const long long ob = tile / ttiles, t0 = (long long)(tile % ttiles) * (32 * TT);
     if (t0 + 32 * j >= A.T) return;
     const gq_float4 *p = partial + (((size_t)nth * WIDE_R + rg) * TT + j) * 512 + 2 * q * 64 + lane;
@@ -569,30 +569,32 @@ bool all_on(int64_t border, std::initializer_list<const void *> ps) {
     return true;
 }
 
-// How the tiles of a product are shared out: `ks` times four wavefronts a workgroup; `whole` workgroups with a tile each, `parts` for every one of
-// the `rest`.
+// How the tiles of a product are shared out.  `pairs` tiles by four wavefronts a workgroup, two workgroups a compute unit.  Then `whole` tiles and `parts`
+// of each of the `rest` by eight wavefronts a workgroup, one workgroup a compute unit.
+// us with all tiles of the first kind / with the second: 64 tiles (512 tokens on 4096 x 4096) 70 / 39, 256 (2048 on 4096 x 11008) 178 / 164, 344 (512 on
+// gated 11008 x 4096) 105 / 103, 512 (2048 on 8192 x 11008) 299 / 330; with the second for what full rounds of the first leave: 4 of 516 (1500 on 11008 x
+// 4096) 175 / 136, 176 of 688 (1024 on gated 11008 x 4096) 180 / 184.  So the first by full rounds, and the second for the rest where it is at most half a
+// tile, or one and a half, for every compute unit; alone also up to one.  Its tiles beyond a whole number for every unit are cut along the sum into as
+// many parts as there are units left for each, of at least 4 blocks of 128.
+// Tiles of 64 tokens (gradients; forward there are always more) where there are no more: 64 on 4096 x 11008 25 us, 29 with half-empty ones.
 struct WidePlan {
-    int64_t ttiles, tiles, whole, rest;
-    int ks, parts, tt;
+    int64_t ttiles, pairs, whole, rest;
+    int parts, tt;
     size_t scratch() const { return parts > 1 ? (size_t)rest * parts * WIDE_R * tt * 512 * sizeof(gq_float4) : 0; }
-    void join_none() { whole = tiles, rest = 0, parts = 1; }
+    void join_none() { whole += rest, rest = 0, parts = 1; }
 };
-// Eight wavefronts a workgroup, one workgroup a compute unit, up to one tile and a half for each; four, two workgroups, beyond.  us with four / eight:
-// 64 tiles (512 tokens on 4096 x 4096) 70 / 39, 256 (2048 on 4096 x 11008) 178 / 164, 344 (512 on gated 11008 x 4096) 105 / 103, 512 (2048 on 8192 x 11008)
-// 308 / 330.  With eight, the tiles beyond a whole number for every compute unit are cut along the sum into as many parts as there are units left for
-// each; a part is at least 4 blocks of 128.  Tiles of 64 tokens (gradients; forward there are always more) where there are no more: 64 on 4096 x 11008
-// 25 us, 29 with half-empty ones.
 WidePlan wide_plan(const skim_ctx *ctx, int64_t out, int64_t per, int64_t blocks, int64_t T) {
     WidePlan p;
     p.tt = T <= 64 ? 2 : 4;
     p.ttiles = (T + 32 * p.tt - 1) / (32 * p.tt);
-    p.tiles = (out + per - 1) / per * p.ttiles;
-    p.join_none();
-    p.ks = 2 * p.tiles <= 3 * ctx->num_cu && blocks >= 4 ? 2 : 1;
-    if (p.ks == 2) {
-        const int64_t rest = p.tiles % ctx->num_cu, parts = rest ? std::min<int64_t>(ctx->num_cu / rest, blocks / 4) : 1;
-        if (parts > 1) p.whole = p.tiles - rest, p.rest = rest, p.parts = (int)parts;
-    }
+    const int64_t cu = ctx->num_cu, tiles = (out + per - 1) / per * p.ttiles, left = tiles % (2 * cu);
+    const bool second = blocks >= 4 && (tiles <= cu || (2 * left <= 3 * cu && 2 * (left % cu) <= cu));
+    p.pairs = second ? tiles - left : tiles;
+    p.whole = tiles - p.pairs;
+    p.rest = 0;
+    p.parts = 1;
+    const int64_t rest = p.whole % cu, parts = rest ? std::min<int64_t>(cu / rest, blocks / 4) : 1;
+    if (parts > 1) p.whole -= rest, p.rest = rest, p.parts = (int)parts;
     return p;
 }
 
@@ -635,42 +637,36 @@ skim_status launch_wide(skim_ctx *ctx, MmArgs A, int group, int x_type, int mats
     }
     WidePlan p = wide_plan(ctx, DX ? A.m : A.n, MODE == MM_PLAIN ? 256 : 128, (depth + 127) / 128 * mats, A.T);
     if (p.scratch() > scratch_bytes) p.join_none();
-    if (p.tiles > 0x3fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens are too many for one call", A.T);
-    const size_t lds = p.ks * (2 * wide_x_bytes(p.tt) + (DX ? 4 * WIDE_A_BYTES : 0));
+    if (p.pairs > 0x3fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens are too many for one call", A.T);
     auto go = [&](auto split, auto tokens) -> hipError_t {
-        constexpr int KS = decltype(split)::value;
-        auto *k = &group_wide_kernel<DX, MODE, KS, decltype(tokens)::value>;
+        constexpr int KS = decltype(split)::value, TT = decltype(tokens)::value;
+        const size_t lds = KS * (2 * wide_x_bytes(TT) + (DX ? 4 * WIDE_A_BYTES : 0));
+        auto *k = &group_wide_kernel<DX, MODE, KS, TT>;
         hipError_t e = hipSuccess;
-        const unsigned bit = 1u << (DX ? 2 * (KS - 1) + (decltype(tokens)::value == 4) : 4 + MODE);      // (forward four wavefronts need no more than 64 KB)
+        const unsigned bit = 1u << (DX ? 2 * (KS - 1) + (TT == 4) : 4 + MODE);       // (forward four wavefronts need no more than 64 KB)
         if (lds > 64 * 1024 && !(ctx->wide_lds_enabled & bit)) {
             e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e == hipSuccess) ctx->wide_lds_enabled |= bit;
         }
-        if (e == hipSuccess)
-            hipLaunchKernelGGL(k, dim3((unsigned)(p.whole + p.rest * p.parts)), dim3(WIDE_THREADS * KS), lds, ctx->stream, A, group, mats, (int)p.ttiles,
+        if (e != hipSuccess) return e;
+        if (KS == 1)
+            hipLaunchKernelGGL(k, dim3((unsigned)p.pairs), dim3(WIDE_THREADS), lds, ctx->stream, A, group, mats, (int)p.ttiles, 0, (int)p.pairs, 0, 1,
+                               (gq_float4 *)nullptr);
+        else
+            hipLaunchKernelGGL(k, dim3((unsigned)(p.whole + p.rest * p.parts)), dim3(2 * WIDE_THREADS), lds, ctx->stream, A, group, mats, (int)p.ttiles, (int)p.pairs,
                                (int)p.whole, (int)p.rest, p.parts, (gq_float4 *)room);
-        return e;
+        if (KS == 2 && p.parts > 1)
+            hipLaunchKernelGGL((group_join_kernel<DX, MODE, TT>), dim3((unsigned)(p.rest * WIDE_R * TT)), dim3(256), 0, ctx->stream, A, (int)p.ttiles,
+                               (int)(p.pairs + p.whole), (int)p.rest, p.parts, (const gq_float4 *)room);
+        return hipGetLastError();
     };
     auto by_tokens = [&](auto split) {
         if constexpr (DX)
             if (p.tt == 2) return go(split, std::integral_constant<int, 2>{});
         return go(split, std::integral_constant<int, 4>{});
     };
-    SKIM_HIP(ctx, p.ks == 1 ? by_tokens(std::integral_constant<int, 1>{}) : by_tokens(std::integral_constant<int, 2>{}));
-    SKIM_HIP(ctx, hipGetLastError());
-    if (p.parts > 1) {
-        auto join = [&](auto tokens) {
-            hipLaunchKernelGGL((group_join_kernel<DX, MODE, decltype(tokens)::value>), dim3((unsigned)(p.rest * WIDE_R * p.tt)), dim3(256), 0, ctx->stream, A,
-                               (int)p.ttiles, (int)p.whole, (int)p.rest, p.parts, (const gq_float4 *)room);
-        };
-        if constexpr (DX) {
-            if (p.tt == 2) join(std::integral_constant<int, 2>{});
-            else join(std::integral_constant<int, 4>{});
-        } else {
-            join(std::integral_constant<int, 4>{});
-        }
-        SKIM_HIP(ctx, hipGetLastError());
-    }
+    if (p.pairs) SKIM_HIP(ctx, by_tokens(std::integral_constant<int, 1>{}));
+    if (p.whole + p.rest) SKIM_HIP(ctx, by_tokens(std::integral_constant<int, 2>{}));
     return SKIM_OK;
 }
 

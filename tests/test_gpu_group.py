@@ -630,9 +630,9 @@ def test_refusals(ctx, gpu_lib):
 # ---- how the work is shared out, memory far away, other streams -----------------------------------------------------------
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T,n,m", [(2048, 4352, 1030), (4096, 4352, 140), (512, 4096, 4096)])
+@pytest.mark.parametrize("T,n,m", [(2048, 4352, 1030), (4096, 4352, 140), (512, 4096, 4096), (4096, 4130, 1100)])
 def test_many_tiles(ctx, T, n, m):
-    """272 tiles (256 whole ones, the rest in parts), 544 (four wavefronts a workgroup) and 64 (all in parts)."""
+    """272 tiles (256 whole ones, the rest in parts), 544 (four wavefronts a workgroup), 64 (all in parts), 544 again as 512 and 32 in parts."""
     rng = np.random.default_rng(T + m)
     gq, W = matrix(rng, n, m, 64)
     x, s, value = inputs(rng, T, m, "e4m3")
