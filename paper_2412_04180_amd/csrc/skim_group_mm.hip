@@ -119,16 +119,17 @@ __device__ __forceinline__ gq_float4 mfma(gq_bf16x8 a, gq_bf16x8 b, gq_float4 c)
 // is a multiple of 8.
 template <int XT>
 struct XOctet {
+    typedef std::conditional_t<XT == SKIM_BF16, uint16_t, uint8_t> E;
     std::conditional_t<XT == SKIM_BF16, gq_word4, gq_word2> v;
+    __device__ __forceinline__ void load_whole(const void *x, long long at) { __builtin_memcpy(&v, (const E *)x + at, sizeof(v)); }      // (one load, of any alignment)
     template <bool VEC>
     __device__ __forceinline__ void load(const void *x, long long row0, long long col, long long m) {
-        typedef std::conditional_t<XT == SKIM_BF16, uint16_t, uint8_t> E;
         const E *p = (const E *)x + row0 + col;
         if constexpr (VEC) {
             if (col < m) v = *(const decltype(v) *)p;
             else v = decltype(v){};
         } else if (col + 8 <= m) {
-            __builtin_memcpy(&v, p, sizeof(v));              // (one load, of any alignment)
+            load_whole(p, 0);
         } else {
             E e[8];
 #pragma unroll
@@ -178,9 +179,15 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const long long t = t0 + 16 * j + l16;
+                const long long col = (long long)kb * GQ_COLS + 8 * c;
                 if (t < A.T) {
+                    if ((long long)(kb + 1) * GQ_COLS <= A.m) {                   // a whole block: nothing to look at lane by lane
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[u][k][j].template load<VEC>(A.x, t * A.ldx, (long long)kb * GQ_COLS + 32 * k + 8 * c, A.m);
+                        for (int k = 0; k < 4; ++k) x[u][k][j].load_whole(A.x, t * A.ldx + col + 32 * k);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[u][k][j].template load<VEC>(A.x, t * A.ldx, col + 32 * k, A.m);
+                    }
                 }
             }
         }
