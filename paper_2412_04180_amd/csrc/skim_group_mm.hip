@@ -147,7 +147,8 @@ struct XOctet {
 
 // A workgroup makes 16 rows of the result for 16 tokens, or (NT = 2) 32 for 32; its wavefronts share the columns block by block, and their sums are added up in
 // LDS in the order of the wavefronts.  Codes enter the matrix cores as whole numbers; a group's sum is multiplied by the scale once.  Bound by
-// the codes' way from memory: a wavefront asks for U blocks at once, with their scales and their columns of x, before it takes the first apart.
+// the codes' way from memory: a wavefront asks for U blocks at once, with their scales and their columns of x, before it takes the first apart.  One
+// token on 4096 x 11008 7.7 us (3.0 TB/s; 13.5 with a block at a time), gated on 11008 x 4096 12.3 (3.8 TB/s); in the registers of a wavefront is room for no more.
 template <int XT, int NT, int G, int MODE, bool VEC>
 __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs A, int chunks) {
     constexpr int RT = NT, MATS = MODE == MM_PLAIN ? 1 : 2, U = NT > 1 ? 1 : MATS * (GQ_COLS / G) * (XT == SKIM_BF16 ? 2 : 1) <= 2 ? 4 : 2, GS = GQ_COLS / G;
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
 // LDS rows of a token are 256 bytes; its 16-byte unit u is at place u ^ (token % 16), so that 16 tokens' units of one column octet lie in different banks.
 // 32 x 32 instructions: half as many as of 16 x 16 for the same product.  No wait stands between a load and the end of its block: a value that is
 // shifted or combined as it arrives is waited for at once, which cost 20 % when it happened to the scales.
-// Bound by the matrix cores and the power they draw: 2048 tokens on 8192 x 11008 run at 1.10-1.22 PFLOP/s (matrix products of bfloat16 matrices at
+// Bound by the matrix cores and the power they draw: 2048 tokens on 8192 x 11008 run at 1.15-1.24 PFLOP/s (matrix products of bfloat16 matrices at
 // 1.45-1.5), on x of zeros at 1.46, without the taking apart at 1.33; two wavefronts a SIMD, 256 registers each, leave no room for tiles that would share it more.
 constexpr int WIDE_R = 4, WIDE_THREADS = 64 * WIDE_R;
 constexpr int wide_x_bytes(int tt) { return 32 * tt * GQ_COLS * 2; }     // of one block: 32 KB for 128 tokens
