@@ -303,7 +303,7 @@ typedef enum { SKIM_F32 = 0, SKIM_BF16 = 1, SKIM_E4M3 = 2 } skim_dtype;
  *
  * skim_group_quantize: W dev, n x m float32, stride ld; finite, and below 2^127 in size.
  * skim_group_unpack: Wq dev float32 n x m, stride m. */
-#define SKIM_GROUP_MAX (1 << 24)
+#define SKIM_GROUP_MAX (1 << 23)
 int64_t skim_group_code_words(int64_t n, int64_t m);
 int64_t skim_group_scale_entries(int64_t n, int64_t m, int group);
 skim_status skim_group_quantize(skim_ctx *ctx, const float *W, int64_t n, int64_t m, int64_t ld, int group, uint32_t *codes,

@@ -20,7 +20,7 @@ STATUS_NAMES = {0: "SKIM_OK", -1: "SKIM_ERR_ARG", -2: "SKIM_ERR_SHAPE", -3: "SKI
                 -4: "SKIM_ERR_WORKSPACE", -5: "SKIM_ERR_HIP", -6: "SKIM_ERR_NONFINITE"}
 MAX_M = 32768
 PACK_STATIC_MAX_ROWS = 65536
-GROUP_MAX = 1 << 24
+GROUP_MAX = 1 << 23
 F32, BF16, E4M3 = 0, 1, 2          # skim_dtype
 
 EXPORTS = ["skim_create", "skim_destroy", "skim_last_error", "skim_workspace_bytes", "skim_set_workspace",
@@ -503,7 +503,7 @@ class Context:
         p, ld, _ = self._rows(W, (t.float32,), m, "group_quantize: W")
         words, entries = int(self.lib.skim_group_code_words(n, m)), int(self.lib.skim_group_scale_entries(n, m, group))
         if words < 0 or entries < 0:
-            raise ValueError("group_quantize: n, m up to 2^24, groups of 32, 64 or 128 columns")
+            raise ValueError("group_quantize: n, m up to 2^23, groups of 32, 64 or 128 columns")
         n16 = (n + 15) // 16 * 16
         codes = self._result(out["codes"] if out else None, (words,), t.int32, "group_quantize: codes")
         scales = self._result(out["scales"] if out else None, (entries // n16, n16), t.bfloat16, "group_quantize: scales")

@@ -606,16 +606,18 @@ WidePlan wide_plan(const skim_ctx *ctx, int64_t out, int64_t per, int64_t blocks
     return p;
 }
 
-// Whether the tiles can copy rows of x as they are.
+// Whether the tiles can copy rows of x as they are.  (A tile's 128 rows lie within the 2^31 bytes that a copy's offset reaches, which also limits the
+// matrices: their widened rows are as long.)
+static_assert(127ll * SKIM_GROUP_MAX * 2 + 2 * GQ_COLS < (1ll << 31));
 bool wide_takes(const void *x, int x_type, int64_t ldx, int64_t depth) {
-    return x_type == SKIM_BF16 && depth % 8 == 0 && ldx % 8 == 0 && ldx < (1 << 23) && all_on(16, {x});
+    return x_type == SKIM_BF16 && depth % 8 == 0 && ldx % 8 == 0 && ldx <= SKIM_GROUP_MAX && all_on(16, {x});
 }
 int64_t wide_columns(int64_t depth) { return (depth + 7) / 8 * 8; }
 size_t widened_bytes(int64_t depth, int64_t T) { return ((size_t)wide_columns(depth) * T * 2 + 255) / 256 * 256; }
 
 skim_status widen_x(skim_ctx *ctx, const void *x, int x_type, int64_t ldx, int64_t T, int64_t depth, void *out) {
     const int64_t columns = wide_columns(depth), groups = (T * (columns / 8) + 255) / 256;
-    if (groups > 0x7fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens of %lld values are too many for one call", (long long)T, (long long)depth);
+    if (groups > 0xffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens of %lld values are too many for one call", (long long)T, (long long)depth);
     if (x_type == SKIM_BF16)
         hipLaunchKernelGGL(group_widen_kernel<SKIM_BF16>, dim3((unsigned)groups), dim3(256), 0, ctx->stream, x, (long long)ldx, (long long)T, (int)depth, (int)columns,
                            (uint16_t *)out);
@@ -643,9 +645,10 @@ skim_status launch_wide(skim_ctx *ctx, MmArgs A, int group, int x_type, int mats
         room += need;
         scratch_bytes -= need;
     }
+    // (a launch has fewer than 2^32 threads)
     WidePlan p = wide_plan(ctx, DX ? A.m : A.n, MODE == MM_PLAIN ? 256 : 128, (depth + 127) / 128 * mats, A.T);
     if (p.scratch() > scratch_bytes) p.join_none();
-    if (p.pairs > 0x3fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens are too many for one call", A.T);
+    if (p.pairs > 0xffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens are too many for one call", A.T);
     auto go = [&](auto split, auto tokens) -> hipError_t {
         constexpr int KS = decltype(split)::value, TT = decltype(tokens)::value;
         const size_t lds = KS * (2 * wide_x_bytes(TT) + (DX ? 4 * WIDE_A_BYTES : 0));

@@ -148,6 +148,13 @@ def test_sizes_of_the_format(lib):
         assert lib.skim_group_scale_entries(64, 64, group) == -1
 
 
+def test_sizes_past_the_reach_of_a_copy_are_refused(lib):
+    most = 1 << 23                                       # a tile's last row begins 127 rows of 2 bytes a value behind its first: below 2^31
+    assert lib.skim_group_code_words(most, 1) == most // 16 * 256 and lib.skim_group_scale_entries(1, most, 64) == 16 * most // 64
+    for n, m in ((most + 1, 4), (4, most + 1), (1 << 24, 4), (4, 1 << 24)):
+        assert lib.skim_group_code_words(n, m) == -1 and lib.skim_group_scale_entries(n, m, 32) == -1
+
+
 def test_calls_without_a_context_are_refused(lib):
     assert lib.skim_group_quantize(None, None, 1, 1, 1, 128, None, None) == -1
     assert lib.skim_group_unpack(None, None, None, 1, 1, 128, None) == -1
@@ -762,3 +769,31 @@ def test_infinities_and_nans_stay_in_their_token(ctx):
         rest = [t for t in range(T) if t != 1]
         close(dx[rest], (dvalue @ W)[rest], 2.0 ** -24 * np.abs(dvalue @ W)[rest] + loss(100) * (np.abs(dvalue) @ np.abs(W))[rest], "dx")
         assert torch.isnan(dx[1]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_sums_over_the_longest_rows(ctx, kind):
+    """2^23 values a token: the last tokens of a tile begin 2.1 GB behind its first."""
+    T, k, few, G = 128, 1 << 23, 16, 128
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    at = torch.cat([torch.arange(0, 100), torch.arange(k // 2 - 50, k // 2 + 50), torch.arange(k - 300, k)]).cuda()
+    x = torch.zeros((T, k), dtype=torch.bfloat16, device="cuda")
+    x[:, at] = torch.randint(-8, 9, (T, at.numel()), device="cuda", generator=gen).to(torch.bfloat16)       # (e4m3 numbers)
+    v = x[:, at].cpu().double().numpy()
+    codes = torch.randint(-2 ** 31, 2 ** 31, (few * k // 8,), dtype=torch.int32, device="cuda", generator=gen)
+    scale = lambda *shape: (torch.randint(16, 32, shape, device="cuda", generator=gen).float() / 1024).to(torch.bfloat16)
+    wide = dict(codes=codes, scales=scale(k // G, few), n=few, m=k, group=G)
+    D = ctx.group_unpack(wide)[:, at].cpu().double().numpy()
+    allowed = lambda D: 2.0 ** -24 * np.abs(v @ D) + loss(at.numel() + 64) * (np.abs(v) @ np.abs(D))          # (zeros add without loss)
+    if kind == "bf16":
+        y = ctx.group_matmul(wide, x, out_dtype=torch.float32)
+    else:
+        y = ctx.group_matmul(wide, x.to(torch.float8_e4m3fn), x_scales=torch.ones(T, device="cuda"), out_dtype=torch.float32)
+    close(y, v @ D.T, allowed(D.T), "y")
+    if kind == "bf16":
+        tall = dict(codes=torch.randint(-2 ** 31, 2 ** 31, (k * 16,), dtype=torch.int32, device="cuda", generator=gen), scales=scale(1, k), n=k, m=few, group=G)
+        D = ctx.group_unpack(tall)[at].cpu().double().numpy()
+        close(ctx.group_matmul_dx(tall, x, out_dtype=torch.float32), v @ D, allowed(D), "dx")
+    del x, wide, codes
+    torch.cuda.empty_cache()
