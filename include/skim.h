@@ -350,9 +350,11 @@ skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *gate_codes, c
 /* Root-mean-square norm, with the residual's addition ahead of it and an 8-bit output for the products above:
  *   h = x + residual (rounded to the type; without a residual h is x),  rstd = 1 / sqrt(mean_j h_j^2 + eps),  y_j = h_j rstd weight_j
  *   scales = max_j |y_j| / 448 (float32, at least 2^-126; 1 for a row of zeros),   q_j = y_j / scales rounded to e4m3, ties to even
- * Statistics and the quotients are float64: q is the rounding of the formula's value.
+ * Statistics and the quotients are float64: q is the rounding of the formula's value.  A row with a NaN or an infinity has a NaN for its scale and
+ * all of its q.
  * x, residual: dev rows x m of `type` (SKIM_BF16 or SKIM_F32), row strides ldx, ldr >= m.  weight: dev float32[m], NULL = 1.
- * h (given with residual and only then; it may be x or residual itself where that is dense), y: dev rows x m of `type`, dense; q: dev
+ * h (given with residual and only then; it may be x or residual itself where that is dense, the other outputs lie apart from all inputs), y: dev rows x
+ * m of `type`, dense; q: dev
  * rows x m bytes with scales dev float32[rows]; rstd: dev float32[rows].  y, q with scales, and rstd may be NULL, not all of them.
  * eps > 0, 1 <= m <= SKIM_MAX_M. */
 skim_status skim_rms_norm(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, int type, const float *weight,
@@ -361,8 +363,8 @@ skim_status skim_rms_norm(skim_ctx *ctx, const void *x, int64_t ldx, const void 
 /* Its backward pass, through y (the rounding to 8 bits passes gradients on unchanged):
  *   with n = h rstd and g = dy weight:   dx = rstd (g - n mean_j(g_j n_j)) + dh,   dweight = sum over the rows of dy n
  * dy: dev rows x m of `type`: the gradient to y; h: what skim_rms_norm wrote (x where there was no residual), rstd likewise; dh: the
- * gradient that reaches h past the norm, NULL = none; row strides lddy, ldh, lddh.  dx: dev rows x m of `type`, dense: the gradient to x, and
- * to the residual.  dweight: dev float32[m], NULL = not wanted; it needs scratch (dev, 4-byte aligned) of
+ * gradient that reaches h past the norm, NULL = none; row strides lddy, ldh, lddh.  dx: dev rows x m of `type`, dense, apart from all inputs: the
+ * gradient to x, and to the residual.  dweight: dev float32[m], NULL = not wanted; it needs scratch (dev, 4-byte aligned) of
  * skim_rms_norm_scratch_bytes(ctx, rows, m) bytes.  Arithmetic in float32, the rows of dweight added in a fixed order. */
 size_t skim_rms_norm_scratch_bytes(const skim_ctx *ctx, int64_t rows, int64_t m);
 skim_status skim_rms_norm_backward(skim_ctx *ctx, const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dh, int64_t lddh,

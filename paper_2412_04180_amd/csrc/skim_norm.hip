@@ -190,8 +190,9 @@ rms_norm_kernel(const T *x, long long ldx, const T *residual, long long ldr, con
             top = fmax(top, red[turn][1][i]);
         }
         const double rstd = 1.0 / sqrt(sum / (double)m + (double)eps);
-        // (a scale below the least normal number would have digits missing; one row of zeros has none: 1)
-        const float scale = top > 0.0 ? fmaxf((float)(top * rstd / E4M3_MAX), 1.17549435e-38f) : 1.f;
+        // (a scale below the least normal number would have digits missing; a row of zeros has none: 1; that of a row with a NaN or an infinity is NaN)
+        const double unit = top * rstd / E4M3_MAX;
+        const float scale = top == 0.0 && unit == 0.0 ? 1.f : unit < 0x1p-126 ? 0x1p-126f : (float)unit;
         if (tid == 0) {
             if (rstd_out) rstd_out[t] = (float)rstd;
             if (q) scales[t] = scale;

@@ -797,3 +797,21 @@ def test_sums_over_the_longest_rows(ctx, kind):
         close(ctx.group_matmul_dx(tall, x, out_dtype=torch.float32), v @ D, allowed(D), "dx")
     del x, wide, codes
     torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("m", [1, 100, 4096, 20000])
+def test_rms_norm_of_rows_with_nans_and_infinities(ctx, dtype, m):
+    x = torch.randn((6, m), device="cuda").to(dtype)
+    good = ctx.rms_norm(x, want_y=True)
+    bad = x.clone()
+    bad[1, m // 2], bad[2, m - 1], bad[4] = float("nan"), float("-inf"), float("nan")
+    o = ctx.rms_norm(bad, want_y=True)
+    for t in range(6):
+        if t in (1, 2, 4):
+            assert torch.isnan(o["scales"][t]) and torch.isnan(o["q"][t].float()).all(), t
+            assert torch.isnan(o["y"][t]).all() if t != 2 else torch.isnan(o["y"][t, -1]) and not o["y"][t, :-1].any()
+        else:
+            for key in ("scales", "q", "y", "rstd"):
+                assert torch.equal(o[key][t].float(), good[key][t].float()), (t, key)
