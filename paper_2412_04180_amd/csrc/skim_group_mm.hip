@@ -30,6 +30,11 @@ struct MmArgs {
     const uint16_t *da;          // backward pass of the gated block
     long long ldda;
     uint16_t *dgate, *dup;
+    // Gradients of few tokens in two pieces.  Written: rows 2 t and 2 t + 1 of dgate and, 2 T rows on, of dup, ldp values each (a multiple of 16, zeros past n).
+    // Read (dx): x and x2 are such rows, T counts them, and a token's result is the sum of its two.
+    uint16_t *pieces;
+    long long ldp;
+    bool paired;
     bool quads;                  // results (and da) can be taken in fours
 };
 
@@ -37,16 +42,26 @@ enum { MM_PLAIN, MM_GLU, MM_GLU_BACK };
 
 __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float from_bf16(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+// What v has beyond its bfloat16 (0 where that is no number to take it from).
+__device__ __forceinline__ uint16_t second_piece(float v, uint16_t first) { return (first & 0x7F80) == 0x7F80 ? (uint16_t)0 : to_bf16(v - from_bf16(first)); }
 __device__ __forceinline__ float sigmoid(float g) { return 1.f / (1.f + expf(-g)); }
 
 // Four neighbouring results of a token, of rows `row` .. row + 3 of `rows`; the token is inside.  Sums come times `by`.
-template <int MODE>
+template <int MODE, bool FEW = false>
 __device__ __forceinline__ void finish4(const MmArgs &A, long long t, long long row, long long rows, gq_float4 g, gq_float4 u, float by) {
-    if (row >= rows) return;
+    if (row >= rows) {
+        if constexpr (MODE == MM_GLU_BACK && FEW) {
+            if (A.pieces && row < A.ldp) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *(gq_short4 *)(A.pieces + ((i >> 1) * 2 * A.T + 2 * t + (i & 1)) * A.ldp + row) = gq_short4{};
+            }
+        }
+        return;
+    }
     const long long at = t * rows + row;
     const bool quad = A.quads;                    // rows come in fours, everything on borders of fours
     if constexpr (MODE == MM_GLU_BACK) {
-        gq_short4 d = {}, dg, du;
+        gq_short4 d = {}, dg, du, dg2 = {}, du2 = {};
         const uint16_t *p = A.da + t * A.ldda + row;
         if (quad) d = *(const gq_short4 *)p;
         else
@@ -54,9 +69,23 @@ __device__ __forceinline__ void finish4(const MmArgs &A, long long t, long long 
                 if (row + i < rows) d[i] = (short)p[i];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            const bool in = row + i < rows;                                // (past the last row the sums are zeros, but for a token with an infinity or a NaN)
             const float gi = g[i] * by, ui = u[i] * by, di = from_bf16((uint16_t)d[i]), s = sigmoid(gi);
-            dg[i] = (short)to_bf16(di * ui * s * fmaf(gi, 1.f - s, 1.f));
-            du[i] = (short)to_bf16(di * gi * s);
+            const float vg = in ? di * ui * s * fmaf(gi, 1.f - s, 1.f) : 0.f, vu = in ? di * gi * s : 0.f;
+            dg[i] = (short)to_bf16(vg);
+            du[i] = (short)to_bf16(vu);
+            if constexpr (FEW) {
+                dg2[i] = (short)second_piece(vg, (uint16_t)dg[i]);
+                du2[i] = (short)second_piece(vu, (uint16_t)du[i]);
+            }
+        }
+        if (FEW && A.pieces) {
+            uint16_t *q = A.pieces + 2 * t * A.ldp + row;
+            *(gq_short4 *)q = dg;
+            *(gq_short4 *)(q + A.ldp) = dg2;
+            q += 2 * A.T * A.ldp;
+            *(gq_short4 *)q = du;
+            *(gq_short4 *)(q + A.ldp) = du2;
         }
         if (quad) {
             *(gq_short4 *)(A.dgate + at) = dg;
@@ -242,7 +271,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
             for (int w = 0; w < nw; ++w) v[a] += red[(w * MATS + a) * E + e];
         const int el = e & 63;
         const long long t = t0 + 16 * ((e >> 6) % NT) + (el & 15), rt = rt0 + (e >> 6) / NT;
-        if (t < A.T) finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
+        if (t < A.T) finish4<MODE, true>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
     }
 }
 
@@ -277,10 +306,23 @@ __device__ __forceinline__ gq_word4 weight_operand(uint32_t w, float s) {
     return v;
 }
 
+// The other lane's of a pair.
+__device__ __forceinline__ float neighbour(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true)); }
+
 // Four sums of either row tile of wavefront `w` (counted through all tiles) for token t, those `in` rows down the tile.
 template <bool DX, int MODE>
 __device__ __forceinline__ void wide_finish(const MmArgs &A, long long w, long long t, int in, gq_float4 v0, gq_float4 v1) {
-    if (t >= A.T) return;
+    if (DX && A.paired) {                            // a token's two rows are two lanes'
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v0[i] += neighbour(v0[i]);
+            v1[i] += neighbour(v1[i]);
+        }
+        if (t >= A.T || (t & 1)) return;
+        t >>= 1;
+    } else if (t >= A.T) {
+        return;
+    }
     const float by = A.x_scales ? A.x_scales[t] : 1.f;
     if constexpr (MODE == MM_PLAIN) {
         finish4<MODE>(A, t, w * 64 + in, DX ? A.m : A.n, v0, gq_float4{}, by);
@@ -615,6 +657,13 @@ bool wide_takes(const void *x, int x_type, int64_t ldx, int64_t depth) {
 int64_t wide_columns(int64_t depth) { return (depth + 7) / 8 * 8; }
 size_t widened_bytes(int64_t depth, int64_t T) { return ((size_t)wide_columns(depth) * T * 2 + 255) / 256 * 256; }
 
+// Of dgate and dup in two pieces: up to PIECES_TO tokens of the gated block's backward pass give dx 16 bits of them, as pairs of rows of the tiles.  So few
+// tokens leave half a tile empty anyway (gated 11008 x 4096: 1 token 45.6 us, 32 59, 64 82, as stored 44.2, 55 and 69), and their errors do not average: dx of rounded
+// gradients is 1.2 to 1.8 times as far off as its own rounding makes it.  For more tokens that is 1.4 times throughout, and the pieces would be twice the
+// products.
+constexpr int64_t PIECES_TO = 64;
+size_t piece_bytes(int64_t n, int64_t T) { return T > PIECES_TO ? 0 : ((size_t)gq_row_blocks(n) * GQ_ROWS * 2 * 2 * T * 2 + 255) / 256 * 256; }
+
 skim_status widen_x(skim_ctx *ctx, const void *x, int x_type, int64_t ldx, int64_t T, int64_t depth, void *out) {
     const int64_t columns = wide_columns(depth), groups = (T * (columns / 8) + 255) / 256;
     if (groups > 0xffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens of %lld values are too many for one call", (long long)T, (long long)depth);
@@ -632,7 +681,8 @@ template <bool DX, int MODE>
 skim_status launch_wide(skim_ctx *ctx, MmArgs A, int group, int x_type, int mats, void *scratch, size_t scratch_bytes) {
     const int64_t depth = DX ? A.n : A.m;
     char *room = (char *)scratch;
-    if (!wide_takes(A.x, x_type, A.ldx, depth) || (mats == 2 && !wide_takes(A.x2, x_type, A.ldx, depth))) {
+    if (A.paired) {                                                  // (rows of ours, zeros past the matrix)
+    } else if (!wide_takes(A.x, x_type, A.ldx, depth) || (mats == 2 && !wide_takes(A.x2, x_type, A.ldx, depth))) {
         const size_t each = widened_bytes(depth, A.T), need = each * mats;
         if (need > scratch_bytes)
             SKIM_FAIL(ctx, SKIM_ERR_WORKSPACE, "%lld tokens of this type, stride or alignment need %zu bytes of scratch, %zu given", A.T, need, scratch_bytes);
@@ -762,6 +812,8 @@ extern "C" size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64
     if (gradients == 0) return forward;
     // to the input: the same for one gradient of any alignment, or two whose rows may not be multiples of 8
     if (gradients == 1) return widened_bytes(n, T) + wide_plan(ctx, m, 256, over_n, T).scratch();
+    const size_t pieces = piece_bytes(n, T);
+    if (pieces) return pieces + wide_plan(ctx, m, 256, 2 * over_n, 2 * T).scratch();
     return std::max(forward, (n % 8 ? 2 * widened_bytes(n, T) : 0) + wide_plan(ctx, m, 256, 2 * over_n, T).scratch());
 }
 
@@ -831,7 +883,13 @@ extern "C" skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *ga
         SKIM_FAIL(ctx, SKIM_ERR_ARG, "%s: dgate and dup must not be NULL, and 16-byte aligned", who);
     MmArgs A = matrix_args(gate_codes, gate_scales, up_codes, up_scales, n, m);
     A.x = x, A.ldx = ldx, A.x_scales = x_scales, A.T = T, A.da = da_bf16, A.ldda = ldda, A.dgate = dgate_bf16, A.dup = dup_bf16;
+    if (dx && piece_bytes(n, T) && piece_bytes(n, T) <= scratch_bytes) A.pieces = (uint16_t *)scratch, A.ldp = gq_row_blocks(n) * GQ_ROWS;
     if ((st = launch_forward<MM_GLU_BACK>(ctx, A, group, x_type, scratch, scratch_bytes)) != SKIM_OK || !dx) return st;
     A.x = dgate_bf16, A.x2 = dup_bf16, A.ldx = n, A.x_scales = nullptr, A.y = dx, A.y_f32 = dx_type == SKIM_F32;
+    if (A.pieces) {
+        A.x = A.pieces, A.x2 = A.pieces + 2 * T * A.ldp, A.ldx = A.ldp, A.T = 2 * T, A.paired = true;
+        scratch = (char *)scratch + piece_bytes(n, T);
+        scratch_bytes -= piece_bytes(n, T);
+    }
     return launch_dx(ctx, A, group, 2, scratch, scratch_bytes);
 }
