@@ -322,8 +322,13 @@ skim_status skim_group_unpack(skim_ctx *ctx, const uint32_t *codes, const uint16
  * the calls reject, and for up to 64 tokens forward).  It takes x in bfloat16 where rows come in e4m3 or off the 16-byte borders, without room for which
  * calls on more than 64 tokens and gradients are refused (SKIM_ERR_WORKSPACE); and partial sums, up to 32 MB, where the results have few tiles and
  * several compute units share one: without room for them the call is slower.  The order of the sums, and so their last digits, depend on
- * that.  And for skim_group_glu_backward on up to 64 tokens, dgate and dup in 16 bits. */
+ * that.  And for skim_group_glu_backward on up to 64 tokens, dgate and dup in 16 bits.
+ * skim_group_scratch_bytes_for: for one call with this x (gradients = 1: dy; its address is looked at, not what is there), type and row stride, and
+ * with dx of this type: no room for a copy of x that is read as it is, and room for dgate and dup in 16 bits also where a float32 dx of more than 64
+ * tokens is made of them. */
 size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients);
+size_t skim_group_scratch_bytes_for(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients, const void *x, int x_type, int64_t ldx,
+                                    int dx_type);
 skim_status skim_group_matmul(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
                               const void *x, int x_type, int64_t ldx, const float *x_scales, int64_t T, void *y, int y_type,
                               void *scratch, size_t scratch_bytes);
@@ -337,8 +342,9 @@ skim_status skim_group_matmul_dx(skim_ctx *ctx, const uint32_t *codes, const uin
  * The backward pass, with fixed matrices, works g = x Wg^T and u = x Wu^T out again (so x is all that has to be kept, 8 bits of it will do):
  *   dgate = da u silu'(g),  dup = da silu(g)      dev T x n bfloat16, dense, 16-byte aligned
  *   dx = dgate Wg + dup Wu                        dev T x m, dense, SKIM_BF16 or SKIM_F32; NULL = not wanted
- * da: dev T x n bfloat16, row stride ldda >= n.  dx is made of 16 bits of dgate and dup for up to 64 tokens with scratch, else of dgate and dup as
- * they are stored.  For x in e4m3 dx is the gradient to the token's row times its scale. */
+ * da: dev T x n bfloat16, row stride ldda >= n.  With scratch, dx is made of 16 bits of dgate and dup where it is float32 (more than 64 tokens: of
+ * skim_group_scratch_bytes_for bytes, and the products to the input are twice as many) and for up to 64 tokens.  Else it is made of dgate and dup as
+ * they are stored, whose rounding makes the error of a bfloat16 dx 1.4 times that of its own.  For x in e4m3 dx is the gradient to the token's row times its scale. */
 skim_status skim_group_glu(skim_ctx *ctx, const uint32_t *gate_codes, const uint16_t *gate_scales, const uint32_t *up_codes,
                            const uint16_t *up_scales, int64_t n, int64_t m, int group, const void *x, int x_type, int64_t ldx,
                            const float *x_scales, int64_t T, void *a, int a_type, void *scratch, size_t scratch_bytes);

@@ -27,7 +27,7 @@ EXPORTS = ["skim_create", "skim_destroy", "skim_last_error", "skim_workspace_byt
            "skim_profile_enable", "skim_profile_last", "skim_validate_enable",
            "skim_error_table", "skim_error_table_lfull", "skim_cluster_rows", "skim_select_allocated", "skim_greedy_allocate", "skim_greedy_allocate_device",
            "skim_dp_allocate_scratch_bytes", "skim_dp_allocate", "skim_kmeans_optimal_scratch_bytes", "skim_kmeans_optimal",
-           "skim_packed_words", "skim_codebook_entries", "skim_pack", "skim_pack_static", "skim_layer_loss", "skim_scale_step", "skim_train_scale", "skim_unpack", "skim_dequant_matvec", "skim_dequant_matvec_f32", "skim_group_code_words", "skim_group_scale_entries", "skim_group_quantize", "skim_group_unpack", "skim_group_scratch_bytes", "skim_group_matmul", "skim_group_matmul_dx",
+           "skim_packed_words", "skim_codebook_entries", "skim_pack", "skim_pack_static", "skim_layer_loss", "skim_scale_step", "skim_train_scale", "skim_unpack", "skim_dequant_matvec", "skim_dequant_matvec_f32", "skim_group_code_words", "skim_group_scale_entries", "skim_group_quantize", "skim_group_unpack", "skim_group_scratch_bytes", "skim_group_scratch_bytes_for", "skim_group_matmul", "skim_group_matmul_dx",
            "skim_group_glu", "skim_group_glu_backward", "skim_rms_norm", "skim_rms_norm_scratch_bytes", "skim_rms_norm_backward",
            "skim_hessian_workspace_bytes", "skim_hessian_from_activations", "skim_hessian_from_activations_scratch"]
 
@@ -104,6 +104,8 @@ def load_library():
         lib.skim_group_unpack.argtypes = [vp, vp, vp, i64, i64, i32, vp]
         lib.skim_group_scratch_bytes.argtypes = [vp, i64, i64, i64, i32]
         lib.skim_group_scratch_bytes.restype = C.c_size_t
+        lib.skim_group_scratch_bytes_for.argtypes = [vp, i64, i64, i64, i32, vp, i32, i64, i32]
+        lib.skim_group_scratch_bytes_for.restype = C.c_size_t
         lib.skim_group_matmul.argtypes = [vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, vp, C.c_size_t]
         lib.skim_group_matmul_dx.argtypes = [vp, vp, vp, i64, i64, i32, vp, i64, i64, vp, i32, vp, C.c_size_t]
         lib.skim_group_glu.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, vp, C.c_size_t]
@@ -484,7 +486,9 @@ class Context:
 
     def _group_scratch(self, n, m, T, to_input):
         """(pointer, bytes, tensor) of the scratch of a product: it goes back to the allocator with this stream's work queued ahead of its next use."""
-        need = self.lib.skim_group_scratch_bytes(self.h, n, m, T, to_input)
+        return self._scratch(self.lib.skim_group_scratch_bytes(self.h, n, m, T, to_input))
+
+    def _scratch(self, need):
         if need == 0:
             return None, 0, None
         scratch = self.empty((need,), self.torch.uint8)
@@ -549,9 +553,10 @@ class Context:
         self._check(self.lib.skim_group_glu(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, a.data_ptr(), yt, sp, sb))
         return a
 
-    def group_glu_backward(self, gate, up, x, da, x_scales=None, want_dx=True, out=None):
+    def group_glu_backward(self, gate, up, x, da, x_scales=None, want_dx=True, out=None, out_dtype=None):
         """Gradients of group_glu for da (bfloat16, shape of its result): dict(dx [T, m], dgate, dup [T, n]), bfloat16.  g and u are
-        worked out again from x."""
+        worked out again from x.  dx in out_dtype float32 is made of 16 bits of dgate and dup; in bfloat16 that is so for up to 64 tokens, more take
+        them as they are returned."""
         t = self.torch
         gc, gs, n, m, group = self._group_pointers(gate)
         uc, us, *shape = self._group_pointers(up)
@@ -563,10 +568,11 @@ class Context:
         out = out or {}
         dgate = self._result(out.get("dgate"), lead + (n,), t.bfloat16, "group_glu_backward: dgate")
         dup = self._result(out.get("dup"), lead + (n,), t.bfloat16, "group_glu_backward: dup")
-        dx = self._result(out.get("dx"), lead + (m,), t.bfloat16, "group_glu_backward: dx") if want_dx else None
-        sp, sb, _keep = self._group_scratch(n, m, T, 2)
+        dtype, dt = self._result_type(out.get("dx"), out_dtype)
+        dx = self._result(out.get("dx"), lead + (m,), dtype, "group_glu_backward: dx") if want_dx else None
+        sp, sb, _keep = self._scratch(self.lib.skim_group_scratch_bytes_for(self.h, n, m, T, 2 if want_dx else 0, xp, xt, ldx, dt))
         self._check(self.lib.skim_group_glu_backward(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, dap, ldda, dgate.data_ptr(),
-                                                     dup.data_ptr(), None if dx is None else dx.data_ptr(), BF16, sp, sb))
+                                                     dup.data_ptr(), None if dx is None else dx.data_ptr(), dt, sp, sb))
         return dict(dx=dx, dgate=dgate, dup=dup)
 
     # -- norm -----------------------------------------------------------------

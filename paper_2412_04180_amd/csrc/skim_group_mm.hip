@@ -30,7 +30,7 @@ struct MmArgs {
     const uint16_t *da;          // backward pass of the gated block
     long long ldda;
     uint16_t *dgate, *dup;
-    // Gradients of few tokens in two pieces.  Written: rows 2 t and 2 t + 1 of dgate and, 2 T rows on, of dup, ldp values each (a multiple of 16, zeros past n).
+    // Gradients in two pieces, 16 bits of them.  Written: rows 2 t and 2 t + 1 of dgate and, 2 T rows on, of dup, ldp values each (a multiple of 16, zeros past n).
     // Read (dx): x and x2 are such rows, T counts them, and a token's result is the sum of its two.
     uint16_t *pieces;
     long long ldp;
@@ -47,10 +47,10 @@ __device__ __forceinline__ uint16_t second_piece(float v, uint16_t first) { retu
 __device__ __forceinline__ float sigmoid(float g) { return 1.f / (1.f + expf(-g)); }
 
 // Four neighbouring results of a token, of rows `row` .. row + 3 of `rows`; the token is inside.  Sums come times `by`.
-template <int MODE, bool FEW = false>
+template <int MODE>
 __device__ __forceinline__ void finish4(const MmArgs &A, long long t, long long row, long long rows, gq_float4 g, gq_float4 u, float by) {
     if (row >= rows) {
-        if constexpr (MODE == MM_GLU_BACK && FEW) {
+        if constexpr (MODE == MM_GLU_BACK) {
             if (A.pieces && row < A.ldp) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) *(gq_short4 *)(A.pieces + ((i >> 1) * 2 * A.T + 2 * t + (i & 1)) * A.ldp + row) = gq_short4{};
@@ -61,7 +61,7 @@ __device__ __forceinline__ void finish4(const MmArgs &A, long long t, long long 
     const long long at = t * rows + row;
     const bool quad = A.quads;                    // rows come in fours, everything on borders of fours
     if constexpr (MODE == MM_GLU_BACK) {
-        gq_short4 d = {}, dg, du, dg2 = {}, du2 = {};
+        gq_short4 d = {}, dg, du, dg2, du2;
         const uint16_t *p = A.da + t * A.ldda + row;
         if (quad) d = *(const gq_short4 *)p;
         else
@@ -74,12 +74,10 @@ __device__ __forceinline__ void finish4(const MmArgs &A, long long t, long long 
             const float vg = in ? di * ui * s * fmaf(gi, 1.f - s, 1.f) : 0.f, vu = in ? di * gi * s : 0.f;
             dg[i] = (short)to_bf16(vg);
             du[i] = (short)to_bf16(vu);
-            if constexpr (FEW) {
-                dg2[i] = (short)second_piece(vg, (uint16_t)dg[i]);
-                du2[i] = (short)second_piece(vu, (uint16_t)du[i]);
-            }
+            dg2[i] = (short)second_piece(vg, (uint16_t)dg[i]);
+            du2[i] = (short)second_piece(vu, (uint16_t)du[i]);
         }
-        if (FEW && A.pieces) {
+        if (A.pieces) {
             uint16_t *q = A.pieces + 2 * t * A.ldp + row;
             *(gq_short4 *)q = dg;
             *(gq_short4 *)(q + A.ldp) = dg2;
@@ -271,7 +269,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
             for (int w = 0; w < nw; ++w) v[a] += red[(w * MATS + a) * E + e];
         const int el = e & 63;
         const long long t = t0 + 16 * ((e >> 6) % NT) + (el & 15), rt = rt0 + (e >> 6) / NT;
-        if (t < A.T) finish4<MODE, true>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
+        if (t < A.T) finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
     }
 }
 
@@ -657,12 +655,13 @@ bool wide_takes(const void *x, int x_type, int64_t ldx, int64_t depth) {
 int64_t wide_columns(int64_t depth) { return (depth + 7) / 8 * 8; }
 size_t widened_bytes(int64_t depth, int64_t T) { return ((size_t)wide_columns(depth) * T * 2 + 255) / 256 * 256; }
 
-// Of dgate and dup in two pieces: up to PIECES_TO tokens of the gated block's backward pass give dx 16 bits of them, as pairs of rows of the tiles.  So few
+// Of dgate and dup in two pieces: dx in float32, and any dx of up to PIECES_TO tokens, is made of 16 bits of them, as pairs of rows of the tiles.  So few
 // tokens leave half a tile empty anyway (gated 11008 x 4096: 1 token 45.6 us, 32 59, 64 82, as stored 44.2, 55 and 69), and their errors do not average: dx of rounded
-// gradients is 1.2 to 1.8 times as far off as its own rounding makes it.  For more tokens that is 1.4 times throughout, and the pieces would be twice the
-// products.
+// gradients is 1.2 to 1.8 times as far off as its own rounding makes it.  For more tokens that is 1.4 times throughout, and the pieces are twice the
+// products (65 tokens 80 us as stored, 100 in pieces; 1024 378 and 614): who wants them asks for float32.
 constexpr int64_t PIECES_TO = 64;
-size_t piece_bytes(int64_t n, int64_t T) { return T > PIECES_TO ? 0 : ((size_t)gq_row_blocks(n) * GQ_ROWS * 2 * 2 * T * 2 + 255) / 256 * 256; }
+bool takes_pieces(int64_t T, int dx_type) { return T <= PIECES_TO || dx_type == SKIM_F32; }
+size_t piece_bytes(int64_t n, int64_t T) { return ((size_t)gq_row_blocks(n) * GQ_ROWS * 2 * 2 * T * 2 + 255) / 256 * 256; }
 
 skim_status widen_x(skim_ctx *ctx, const void *x, int x_type, int64_t ldx, int64_t T, int64_t depth, void *out) {
     const int64_t columns = wide_columns(depth), groups = (T * (columns / 8) + 255) / 256;
@@ -803,18 +802,37 @@ MmArgs matrix_args(const uint32_t *codes, const uint16_t *scales, const uint32_t
 
 }  // namespace
 
-extern "C" size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients) {
-    if (!ctx || n < 1 || n > SKIM_GROUP_MAX || m < 1 || m > SKIM_GROUP_MAX || T < 1 || T > 0x7fffffff || gradients < 0 || gradients > 2) return 0;
+namespace {
+
+bool sizes_taken(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients) {
+    return ctx && n >= 1 && n <= SKIM_GROUP_MAX && m >= 1 && m <= SKIM_GROUP_MAX && T >= 1 && T <= 0x7fffffff && gradients >= 0 && gradients <= 2;
+}
+// `convert`: x (to the input: its gradient) goes to the tiles through a copy of its own.
+size_t scratch_bytes_of(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients, bool convert, int dx_type) {
     const int64_t over_m = (m + 127) / 128, over_n = (n + 127) / 128;
-    // forward: x in another type or alignment, and the partial sums
+    // forward: that copy, and the partial sums
     const size_t forward = T < WIDE_FROM ? 0
-                                         : widened_bytes(m, T) + std::max(wide_plan(ctx, n, 256, over_m, T).scratch(), wide_plan(ctx, n, 128, over_m, T).scratch());
+                                         : (convert ? widened_bytes(m, T) : 0) +
+                                               std::max(wide_plan(ctx, n, 256, over_m, T).scratch(), wide_plan(ctx, n, 128, over_m, T).scratch());
     if (gradients == 0) return forward;
-    // to the input: the same for one gradient of any alignment, or two whose rows may not be multiples of 8
-    if (gradients == 1) return widened_bytes(n, T) + wide_plan(ctx, m, 256, over_n, T).scratch();
-    const size_t pieces = piece_bytes(n, T);
-    if (pieces) return pieces + wide_plan(ctx, m, 256, 2 * over_n, 2 * T).scratch();
+    // to the input: the same for one gradient, or for two whose rows may not be multiples of 8
+    if (gradients == 1) return (convert ? widened_bytes(n, T) : 0) + wide_plan(ctx, m, 256, over_n, T).scratch();
+    if (takes_pieces(T, dx_type)) return piece_bytes(n, T) + std::max(forward, wide_plan(ctx, m, 256, 2 * over_n, 2 * T).scratch());
     return std::max(forward, (n % 8 ? 2 * widened_bytes(n, T) : 0) + wide_plan(ctx, m, 256, 2 * over_n, T).scratch());
+}
+
+}  // namespace
+
+extern "C" size_t skim_group_scratch_bytes(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients) {
+    return sizes_taken(ctx, n, m, T, gradients) ? scratch_bytes_of(ctx, n, m, T, gradients, true, SKIM_BF16) : 0;
+}
+
+extern "C" size_t skim_group_scratch_bytes_for(const skim_ctx *ctx, int64_t n, int64_t m, int64_t T, int gradients, const void *x, int x_type, int64_t ldx,
+                                               int dx_type) {
+    const int64_t columns = gradients == 1 ? n : m;
+    if (!sizes_taken(ctx, n, m, T, gradients) || (x_type != SKIM_BF16 && (x_type != SKIM_E4M3 || gradients == 1)) || ldx < columns) return 0;
+    if (gradients && dx_type != SKIM_BF16 && dx_type != SKIM_F32) return 0;
+    return scratch_bytes_of(ctx, n, m, T, gradients, !wide_takes(x, x_type, ldx, columns), dx_type);
 }
 
 extern "C" skim_status skim_group_matmul(skim_ctx *ctx, const uint32_t *codes, const uint16_t *scales_bf16, int64_t n, int64_t m, int group,
@@ -883,13 +901,15 @@ extern "C" skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *ga
         SKIM_FAIL(ctx, SKIM_ERR_ARG, "%s: dgate and dup must not be NULL, and 16-byte aligned", who);
     MmArgs A = matrix_args(gate_codes, gate_scales, up_codes, up_scales, n, m);
     A.x = x, A.ldx = ldx, A.x_scales = x_scales, A.T = T, A.da = da_bf16, A.ldda = ldda, A.dgate = dgate_bf16, A.dup = dup_bf16;
-    if (dx && piece_bytes(n, T) && piece_bytes(n, T) <= scratch_bytes) A.pieces = (uint16_t *)scratch, A.ldp = gq_row_blocks(n) * GQ_ROWS;
+    // (the pieces where there is room for them next to the copy of x that the projections cannot do without)
+    const size_t pieces = dx && takes_pieces(T, dx_type) ? piece_bytes(n, T) : 0;
+    if (pieces && pieces + (T < WIDE_FROM || wide_takes(x, x_type, ldx, m) ? 0 : widened_bytes(m, T)) <= scratch_bytes) {
+        A.pieces = (uint16_t *)scratch, A.ldp = gq_row_blocks(n) * GQ_ROWS;
+        scratch = (char *)scratch + pieces;
+        scratch_bytes -= pieces;
+    }
     if ((st = launch_forward<MM_GLU_BACK>(ctx, A, group, x_type, scratch, scratch_bytes)) != SKIM_OK || !dx) return st;
     A.x = dgate_bf16, A.x2 = dup_bf16, A.ldx = n, A.x_scales = nullptr, A.y = dx, A.y_f32 = dx_type == SKIM_F32;
-    if (A.pieces) {
-        A.x = A.pieces, A.x2 = A.pieces + 2 * T * A.ldp, A.ldx = A.ldp, A.T = 2 * T, A.paired = true;
-        scratch = (char *)scratch + piece_bytes(n, T);
-        scratch_bytes -= piece_bytes(n, T);
-    }
+    if (A.pieces) A.x = A.pieces, A.x2 = A.pieces + 2 * T * A.ldp, A.ldx = A.ldp, A.T = 2 * T, A.paired = true;
     return launch_dx(ctx, A, group, 2, scratch, scratch_bytes);
 }

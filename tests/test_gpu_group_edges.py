@@ -1,0 +1,110 @@
+"""Products with 4-bit weights and the norm at the borders of what they are documented for: gradients in 16 bits, strides of every input, scratch of just
+the size that a call needs, values at the ends of the types' ranges.  Plain float64 on the CPU; U and loss() are derived in test_gpu_group.py."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_group import U, ctx, close, dense, dsilu, glu_errors, gradient, inputs, lib, loss, matrix, pack, quantise, silu, weights  # noqa: F401
+
+BF16 = torch.bfloat16
+
+
+# ---- CPU ----------------------------------------------------------------------------------------------------------------
+
+def test_size_of_the_scratch_without_a_context(lib):
+    assert lib.skim_group_scratch_bytes_for(None, 128, 128, 100, 0, None, 1, 128, 1) == 0
+
+
+# ---- gradients of the gated block -----------------------------------------------------------------------------------------
+
+def gated_gradients(value, dav, Wg, Wu, m):
+    """dgate and dup by the formula, and how far float32 ones may be off (as in test_glu_backward; before any rounding to bfloat16)."""
+    g, u, eg, eu = glu_errors(value, Wg, Wu, m)
+    dg, du = dav * u * dsilu(g), dav * silu(g)
+    f = (8 + np.minimum(np.abs(g), 100)) * 2.0 ** -24
+    eg, eu = (np.abs(dav) * (1.1 * eu + 0.5 * eg * (np.abs(u) + eu) + 16 * 2.0 ** -24 * (1 + np.abs(g)) * np.abs(u)) + f * np.abs(dg),
+              np.abs(dav) * 1.1 * eg + f * np.abs(du))
+    return dg, du, eg, eu
+
+
+GATED = [(65, 48, 300, 64), (100, 200, 300, 32), (128, 1021, 500, 128), (130, 272, 1100, 128), (300, 513, 520, 64), (1000, 330, 260, 128)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,n,m,group", GATED)
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_float32_gradients_of_many_tokens_are_rounded_once(ctx, T, n, m, group, kind):
+    """dx in float32 is made of two bfloat16 pieces of dgate and dup, 2^-16 of them off; dgate and dup stay what they are without it."""
+    rng = np.random.default_rng(T + n)
+    (gate, Wg), (up, Wu) = matrix(rng, n, m, group), matrix(rng, n, m, group)
+    x, s, value = inputs(rng, T, m, kind)
+    da, dav = gradient(rng, T, n)
+    o = ctx.group_glu_backward(gate, up, x, da, x_scales=s, out_dtype=torch.float32)
+    dg, du, eg, eu = gated_gradients(value, dav, Wg, Wu, m)
+    want, size = dg @ Wg + du @ Wu, np.abs(dg) @ np.abs(Wg) + np.abs(du) @ np.abs(Wu)
+    off = (eg + 2.0 ** -16 * np.abs(dg)) @ np.abs(Wg) + (eu + 2.0 ** -16 * np.abs(du)) @ np.abs(Wu)
+    assert o["dx"].dtype == torch.float32
+    close(o["dx"], want, 1.01 * off + loss(4 * n) * 1.01 * size + 2.0 ** -24 * np.abs(want), "dx")
+    plain = ctx.group_glu_backward(gate, up, x, da, x_scales=s)
+    assert plain["dx"].dtype == BF16 and torch.equal(plain["dgate"], o["dgate"]) and torch.equal(plain["dup"], o["dup"])
+    into = torch.empty_like(o["dx"])                          # a given result says its type
+    assert ctx.group_glu_backward(gate, up, x, da, x_scales=s, out=dict(dx=into))["dx"] is into and torch.equal(into, o["dx"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,n,m,group", GATED)
+def test_gradients_of_many_tokens_against_the_formula(ctx, T, n, m, group):
+    """dx in bfloat16 is made of dgate and dup as they are returned: two roundings of at most U, each of at most U / sqrt(3) in the root of the mean square; the errors
+    of the first are independent of one another and of the second, so that over the T m results they add up in squares (5 % more allowed for their number)."""
+    rng = np.random.default_rng(T * 3 + n)
+    (gate, Wg), (up, Wu) = matrix(rng, n, m, group), matrix(rng, n, m, group)
+    x, s, value = inputs(rng, T, m, "bf16")
+    da, dav = gradient(rng, T, n)
+    got = ctx.group_glu_backward(gate, up, x, da)["dx"].cpu().double().numpy()
+    dg, du, eg, eu = gated_gradients(value, dav, Wg, Wu, m)
+    want, size = dg @ Wg + du @ Wu, np.abs(dg) @ np.abs(Wg) + np.abs(du) @ np.abs(Wu)
+    u = U[BF16] * 1.01
+    off = (eg + u * np.abs(dg)) @ np.abs(Wg) + (eu + u * np.abs(du)) @ np.abs(Wu) + loss(4 * n) * 1.01 * size
+    assert np.all(np.abs(got - want) <= off + u * (np.abs(want) + off))
+    assert np.linalg.norm(got - want) <= 1.05 * np.sqrt(2 / 3) * U[BF16] * np.linalg.norm(want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [64, 65, 130])
+@pytest.mark.parametrize("kind,ld,offset", [("bf16", 320, 0), ("bf16", 305, 3), ("e4m3", 304, 0)])
+def test_scratch_of_float32_gradients_is_what_the_size_query_says(ctx, T, kind, ld, offset):
+    """Nothing behind it is written; with less, dx is made of dgate and dup as they are stored; a token with a NaN does not reach the others."""
+    rng = np.random.default_rng(T + ld)
+    n, m, group = 208, 300, 64
+    (gate, Wg), (up, Wu) = matrix(rng, n, m, group), matrix(rng, n, m, group)
+    x, s, value = inputs(rng, T, m, kind, ld, offset)
+    value[T - 1, 5] = np.nan
+    x.view(torch.int16 if kind == "bf16" else torch.uint8)[T - 1, 5] = 0x7FC0 if kind == "bf16" else 0x7F
+    da, dav = gradient(rng, T, n)
+    dgate, dup = (torch.empty((T, n), dtype=BF16, device="cuda") for _ in range(2))
+    dx = torch.empty((T, m), device="cuda")
+    xt, sp = (1, None) if kind == "bf16" else (2, s.data_ptr())
+    query = lambda dt: ctx.lib.skim_group_scratch_bytes_for(ctx.h, n, m, T, 2, x.data_ptr(), xt, ld, dt)  # noqa: E731
+    need = query(0)
+    assert need >= 8 * T * n and (T <= 64 or query(1) < need)
+    scratch = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device="cuda")       # (NaN wherever it is not written)
+    mats = [gate["codes"].data_ptr(), gate["scales"].data_ptr(), up["codes"].data_ptr(), up["scales"].data_ptr(), n, m, group]
+
+    def call(room):
+        assert ctx.lib.skim_group_glu_backward(ctx.h, *mats, x.data_ptr(), xt, ld, sp, T, da.data_ptr(), n, dgate.data_ptr(), dup.data_ptr(), dx.data_ptr(), 0,
+                                               scratch.data_ptr(), room) == 0
+        return dx.cpu().double().numpy()
+
+    got = call(need)
+    assert (scratch[need:] == 0xFF).all()
+    dg, du, eg, eu = gated_gradients(value, dav, Wg, Wu, m)
+    want, size = dg @ Wg + du @ Wu, np.abs(dg) @ np.abs(Wg) + np.abs(du) @ np.abs(Wu)
+    off = (eg + 2.0 ** -16 * np.abs(dg)) @ np.abs(Wg) + (eu + 2.0 ** -16 * np.abs(du)) @ np.abs(Wu) + loss(4 * n) * 1.01 * size
+    assert np.all((np.abs(got - want) <= 1.01 * off + 2.0 ** -24 * np.abs(want))[: T - 1]) and np.isnan(got[T - 1]).all()
+    if T > 64:
+        got = call(query(1))
+        sg, su = dgate.cpu().double().numpy(), dup.cpu().double().numpy()
+        over = np.abs(got - (sg @ Wg + su @ Wu)) - loss(2 * n) * (np.abs(sg) @ np.abs(Wg) + np.abs(su) @ np.abs(Wu))
+        assert np.all(over[: T - 1] <= 0) and np.isnan(got[T - 1]).all()
