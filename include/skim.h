@@ -357,7 +357,7 @@ skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *gate_codes, c
  *   h = x + residual (rounded to the type; without a residual h is x),  rstd = 1 / sqrt(mean_j h_j^2 + eps),  y_j = h_j rstd weight_j
  *   scales = max_j |y_j| / 448 (float32, at least 2^-126; 1 for a row of zeros),   q_j = y_j / scales rounded to e4m3, ties to even
  * Statistics and the quotients are float64: q is the rounding of the formula's value.  A row with a NaN or an infinity has a NaN for its scale and
- * all of its q.
+ * all of its q, whatever the weights are, and so has a row with an h_j weight_j that is a NaN (all rows, if a weight is).
  * x, residual: dev rows x m of `type` (SKIM_BF16 or SKIM_F32), row strides ldx, ldr >= m.  weight: dev float32[m], NULL = 1.
  * h (given with residual and only then; it may be x or residual itself where that is dense, the other outputs lie apart from all inputs), y: dev rows x
  * m of `type`, dense; q: dev

@@ -152,6 +152,7 @@ rms_norm_kernel(const T *x, long long ldx, const T *residual, long long ldr, con
     int turn = 0;
     for (long long t = blockIdx.x; t < rows; t += gridDim.x, turn ^= 1) {
         double sum = 0.0, top = 0.0;
+        bool none = false;                               // a product that is no number (also of finite x: with a weight that is not; or 0 times an infinity)
         if (!AHEAD) load_row(t);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -168,7 +169,8 @@ rms_norm_kernel(const T *x, long long ldx, const T *residual, long long ldr, con
             for (int i = 0; i < 8; ++i) {
                 const double d = (double)v[r][i], e = d * (double)w[r][i];
                 sum = fma(d, d, sum);
-                top = fmax(top, fabs(e));
+                top = fmax(top, fabs(e));                // (passes NaNs over)
+                none |= e != e;
                 if (KEEP_P) p[r][i] = e;
             }
         }
@@ -179,19 +181,24 @@ rms_norm_kernel(const T *x, long long ldx, const T *residual, long long ldr, con
             sum += __shfl_xor(sum, d, 64);
             top = fmax(top, __shfl_xor(top, d, 64));
         }
+        const bool some = __any(none);
         if ((tid & 63) == 0) {                           // (two sets: a row's are read while the next row's are written)
             red[turn][0][tid >> 6] = sum;
-            red[turn][1][tid >> 6] = top;
+            red[turn][1][tid >> 6] = some ? __builtin_nan("") : top;
         }
         __syncthreads();
         sum = top = 0.0;
+        none = false;
         for (int i = 0; i < nth / 64; ++i) {
+            const double o = red[turn][1][i];
             sum += red[turn][0][i];
-            top = fmax(top, red[turn][1][i]);
+            top = fmax(top, o);
+            none |= o != o;
         }
         const double rstd = 1.0 / sqrt(sum / (double)m + (double)eps);
-        // (a scale below the least normal number would have digits missing; a row of zeros has none: 1; that of a row with a NaN or an infinity is NaN)
-        const double unit = top * rstd / E4M3_MAX;
+        // (a scale below the least normal number would have digits missing; a row of zeros has none: 1; that of a row with a NaN or an infinity is NaN, and
+        // so is one with a product that is none)
+        const double unit = none ? __builtin_nan("") : top * rstd / E4M3_MAX;
         const float scale = top == 0.0 && unit == 0.0 ? 1.f : unit < 0x1p-126 ? 0x1p-126f : (float)unit;
         if (tid == 0) {
             if (rstd_out) rstd_out[t] = (float)rstd;

@@ -108,3 +108,49 @@ def test_scratch_of_float32_gradients_is_what_the_size_query_says(ctx, T, kind, 
         sg, su = dgate.cpu().double().numpy(), dup.cpu().double().numpy()
         over = np.abs(got - (sg @ Wg + su @ Wu)) - loss(2 * n) * (np.abs(sg) @ np.abs(Wg) + np.abs(su) @ np.abs(Wu))
         assert np.all(over[: T - 1] <= 0) and np.isnan(got[T - 1]).all()
+
+
+# ---- norm -----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,m", [(5, 100), (600, 1000), (600, 4097), (5, 9000), (5, 20000)])
+def test_rms_norm_scales_of_products_that_are_no_numbers(ctx, dtype, T, m):
+    """max |y| / 448 is a NaN where a y is: an infinity under a weight of 0, a weight that is a NaN, 0 under an infinite weight."""
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    x = torch.randn((T, m), device="cuda", generator=gen).to(dtype)
+    w = 1 + 0.1 * torch.randn(m, device="cuda", generator=gen)
+    same = lambda o, ref, rows: all(torch.equal(o[k][rows].float(), ref[k][rows].float()) for k in ("scales", "q", "rstd"))  # noqa: E731
+    no_number = lambda o, t: bool(torch.isnan(o["scales"][t]) and torch.isnan(o["q"][t].float()).all())  # noqa: E731
+    others = [t for t in range(T) if t not in (1, T - 1)]
+    for col in (0, m // 2, m - 1):
+        pruned = w.clone()
+        pruned[col] = 0
+        bad = x.clone()
+        bad[1, col], bad[T - 1, col] = float("inf"), float("-inf")
+        o, ref = ctx.rms_norm(bad, pruned), ctx.rms_norm(x, pruned)
+        assert no_number(o, 1) and no_number(o, T - 1) and same(o, ref, others), col
+        o = ctx.rms_norm(bad, torch.zeros_like(w))             # ... alone: all other products are zeros
+        assert no_number(o, 1) and no_number(o, T - 1) and (o["scales"][others] == 1).all() and not o["q"][others].float().any()
+        without = w.clone()
+        without[col] = float("nan")
+        o = ctx.rms_norm(x, without)
+        assert all(no_number(o, t) for t in range(0, T, max(1, T // 7))) and torch.isnan(o["scales"]).all()
+        assert torch.equal(o["rstd"], ref["rstd"])
+        endless, zero = w.clone(), x.clone()
+        endless[col] = float("inf")
+        zero[:, col] = 1
+        zero[1, col] = zero[T - 1, col] = 0
+        o = ctx.rms_norm(zero, endless)
+        assert no_number(o, 1) and no_number(o, T - 1)
+        assert torch.isinf(o["scales"][others]).all() and torch.isnan(o["q"][others, col].float()).all()
+        rest = o["q"].float()[others]
+        rest[:, col] = 0
+        assert not rest.any()
+    h, r = x.clone(), x.clone()                                # x + residual past the largest number, under a weight of 0
+    big = torch.finfo(dtype).max
+    pruned = w.clone()
+    pruned[7] = 0
+    h[1, 7] = r[1, 7] = big
+    o = ctx.rms_norm(h, pruned, residual=r)
+    assert torch.isinf(o["h"][1, 7]) and no_number(o, 1) and same(o, ctx.rms_norm(x, pruned, residual=x), [t for t in range(T) if t != 1])
