@@ -159,6 +159,9 @@ rms_norm_kernel(const T *x, long long ldx, const T *residual, long long ldr, con
             const int c = (r * nth + tid) * NORM_OCTET;
             v[r] = xr[r].get();
             if (!KEEP) w[r] = load_weight(r);
+            // (kept as float32: the compiler would convert kept weights once for all rows, which with two octets a thread spills 12 to 96 bytes a lane; with the
+            // conversion in the loop 8192 x 4096 bfloat16 52.6 -> 50.5 us, 1024 x 11008 float32 53 -> 38)
+            if (!KEEP_P) asm("" : "+v"(w[r]));
             if (residual) {
                 const float8v e = er[r].get();
 #pragma unroll
