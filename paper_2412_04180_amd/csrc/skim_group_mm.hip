@@ -120,13 +120,26 @@ __device__ __forceinline__ void finish4(const MmArgs &A, long long t, long long 
 
 // ---- operands ------------------------------------------------------------------------------------------------------------
 
-// The codes of a word, whole numbers in bfloat16.
-__device__ __forceinline__ gq_bf16x8 code_operand(uint32_t w) {
+// Scaled weights of a word, exact in bfloat16.
+__device__ __forceinline__ gq_word4 weight_operand(uint32_t w, float s) {
+    gq_word4 v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t bytes = h ? gq_high(w) : gq_low(w);
+        const gq_float2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, true);
+        v[2 * h] = __builtin_amdgcn_perm(__float_as_uint(s * a.y), __float_as_uint(s * a.x), 0x07060302u);
+        v[2 * h + 1] = __builtin_amdgcn_perm(__float_as_uint(s * b.y), __float_as_uint(s * b.x), 0x07060302u);
+    }
+    return v;
+}
+
+// The codes of a word times 2^-9 of a power of two, in bfloat16.
+__device__ __forceinline__ gq_bf16x8 code_operand(uint32_t w, float power) {
     const uint32_t lo = gq_low(w), hi = gq_high(w);
-    const gq_word4 u{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, false)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 512.f, true)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, false)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.f, true))};
+    const gq_word4 u{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true))};
     return __builtin_bit_cast(gq_bf16x8, u);
 }
 
@@ -173,12 +186,20 @@ struct XOctet {
 // ---- few tokens ----------------------------------------------------------------------------------------------------------
 
 // A workgroup makes 16 rows of the result for 16 tokens, or (NT = 2) 32 for 32; its wavefronts share the columns block by block, and their sums are added up in
-// LDS in the order of the wavefronts.  Codes enter the matrix cores as whole numbers; a group's sum is multiplied by the scale once.  Bound by
-// the codes' way from memory: a wavefront asks for U blocks at once, with their scales and their columns of x, before it takes the first apart.  One
-// token on 4096 x 11008 7.7 us (3.0 TB/s; 13.5 with a block at a time), gated on 11008 x 4096 12.3 (3.8 TB/s); in the registers of a wavefront is room for no more.
+// LDS in the order of the wavefronts.  Bound by the codes' way from memory: with up to 16 tokens a wavefront asks for U blocks at once, with their scales and
+// their columns of x, before it takes the first apart.  One token on 4096 x 11008 7.8 us (3.0 TB/s; 13.5 with a block at a time), gated on 11008 x 4096 12.6
+// (3.7 TB/s); in the 128 registers of its wavefronts is room for no more.
+// A scale s is a power of two times its significand in 1/2 .. 1.  Up to 16 tokens (LATE) codes enter the matrix cores times that power, which their conversion brings along
+// for nothing, and a group's sum is multiplied by the significand once: no sum overflows that the formula's does not (sums of q x alone do, for x above 2^118), and
+// the power is 2^-8 of itself so that a scale of 2^124 finds room in the conversion's, exact down to the least scale (q 2^-133, a bfloat16).  x is the first operand there: a lane's
+// four sums are of one row then, and take one significand.  More tokens take weights times scales, as the tiles do.  us the one way / the other: one token on
+// 4096 x 11008 7.8 / 8.6, gated on 11008 x 4096 12.6 / 14.4; 32 tokens on 4096 x 11008 with groups of 32 29 / 25.5, gated 64 36 / 33.
+constexpr int FEW_SHIFT = 8;
+constexpr int FEW_TOKEN = 20;         // floats of a token's 16 rows in LDS: so that 64 lanes' of one access lie in different banks
 template <int XT, int NT, int G, int MODE, bool VEC>
 __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs A, int chunks) {
     constexpr int RT = NT, MATS = MODE == MM_PLAIN ? 1 : 2, U = NT > 1 ? 1 : MATS * (GQ_COLS / G) * (XT == SKIM_BF16 ? 2 : 1) <= 2 ? 4 : 2, GS = GQ_COLS / G;
+    constexpr bool LATE = NT == 1;
     extern __shared__ __align__(16) unsigned char few_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
     const int c = lane >> 4, l16 = lane & 15;
@@ -190,7 +211,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
     gq_float4 acc[MATS][RT][NT] = {};
     for (int first = wave; first < kbs; first += nw * U) {
         gq_word4 w[U][MATS][RT];
-        gq_word2 s[U][MATS][RT][GS];
+        uint32_t s[U][MATS][RT][GS];                                               // of the lane's row
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int kb = first + u * nw;
@@ -202,7 +223,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
                     const long long rt = min(rt0 + r, rbs - 1);
                     w[u][a][r] = A.codes[a][(rt * kbs + kb) * 64 + lane];
 #pragma unroll
-                    for (int g = 0; g < GS; ++g) s[u][a][r][g] = *(const gq_word2 *)(A.scales[a] + ((long long)kb * GS + g) * n16 + rt * GQ_ROWS + 4 * c);
+                    for (int g = 0; g < GS; ++g) s[u][a][r][g] = A.scales[a][((long long)kb * GS + g) * n16 + rt * GQ_ROWS + l16];
                 }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -224,52 +245,68 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
             if (first + u * nw >= kbs) continue;
 #pragma unroll
             for (int g = 0; g < GS; ++g) {
-                gq_float4 d[MATS][RT][NT] = {};
+                gq_float4 d[MATS] = {};
+                float power[MATS];
+                if constexpr (LATE) {
+#pragma unroll
+                    for (int a = 0; a < MATS; ++a) power[a] = ldexpf(1.f, __builtin_amdgcn_frexp_expf(gq_scale(s[u][a][0][g])) + 9 - FEW_SHIFT);
+                }
 #pragma unroll
                 for (int k = g * (4 / GS); k < (g + 1) * (4 / GS); ++k) {
                     gq_bf16x8 b[NT];
 #pragma unroll
                     for (int j = 0; j < NT; ++j) b[j] = x[u][k][j].operand();
 #pragma unroll
-                    for (int a = 0; a < MATS; ++a)
+                    for (int a = 0; a < MATS; ++a) {
+                        if constexpr (LATE) {
+                            d[a] = mfma(b[0], code_operand(w[u][a][0][k], power[a]), d[a]);
+                        } else {
 #pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            const gq_bf16x8 q = code_operand(w[u][a][r][k]);
+                            for (int r = 0; r < RT; ++r) {
+                                const gq_bf16x8 q = __builtin_bit_cast(gq_bf16x8, weight_operand(w[u][a][r][k], gq_scale(s[u][a][r][g])));
 #pragma unroll
-                            for (int j = 0; j < NT; ++j) d[a][r][j] = mfma(q, b[j], d[a][r][j]);
+                                for (int j = 0; j < NT; ++j) acc[a][r][j] = mfma(q, b[j], acc[a][r][j]);
+                            }
                         }
-                }
-#pragma unroll
-                for (int a = 0; a < MATS; ++a)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const gq_word2 v = s[u][a][r][g];
-                        const gq_float4 f{gq_scale(v[0] & 0xFFFF), __uint_as_float(v[0] & 0xFFFF0000u), gq_scale(v[1] & 0xFFFF), __uint_as_float(v[1] & 0xFFFF0000u)};
-#pragma unroll
-                        for (int j = 0; j < NT; ++j)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[a][r][j][i] = fmaf(f[i], d[a][r][j][i], acc[a][r][j][i]);
                     }
+                }
+                if constexpr (LATE) {
+#pragma unroll
+                    for (int a = 0; a < MATS; ++a) {
+                        const float f = __builtin_amdgcn_frexp_mantf(gq_scale(s[u][a][0][g]));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[a][0][0][i] = fmaf(f, d[a][i], acc[a][0][0][i]);
+                    }
+                }
             }
         }
     }
-    constexpr int E = RT * NT * 64;      // fours of a wavefront's sums, for one matrix
+    constexpr int E = RT * NT * 64;      // fours of a wavefront's sums, for one matrix: of 4 rows of a token each
+    constexpr int ROOM = LATE ? 16 * FEW_TOKEN / 4 : E;
     gq_float4 *red = (gq_float4 *)few_lds;
+    if constexpr (LATE) {                // (a lane has 4 tokens of its row)
 #pragma unroll
-    for (int a = 0; a < MATS; ++a)
+        for (int a = 0; a < MATS; ++a)
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+            for (int i = 0; i < 4; ++i) ((float *)(red + (wave * MATS + a) * ROOM))[(4 * c + i) * FEW_TOKEN + l16] = acc[a][0][0][i];
+    } else {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) red[(wave * MATS + a) * E + (r * NT + j) * 64 + lane] = acc[a][r][j];
+        for (int a = 0; a < MATS; ++a)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) red[(wave * MATS + a) * ROOM + (r * NT + j) * 64 + lane] = acc[a][r][j];
+    }
     __syncthreads();
     for (int e = tid; e < E; e += blockDim.x) {
         gq_float4 v[MATS] = {};
+        const int el = e & 63, at = LATE ? (el & 15) * (FEW_TOKEN / 4) + (el >> 4) : e;
 #pragma unroll
         for (int a = 0; a < MATS; ++a)
-            for (int w = 0; w < nw; ++w) v[a] += red[(w * MATS + a) * E + e];
-        const int el = e & 63;
+            for (int w = 0; w < nw; ++w) v[a] += red[(w * MATS + a) * ROOM + at];
         const long long t = t0 + 16 * ((e >> 6) % NT) + (el & 15), rt = rt0 + (e >> 6) / NT;
-        if (t < A.T) finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
+        if (t < A.T)
+            finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], (XT == SKIM_E4M3 ? A.x_scales[t] : 1.f) * (LATE ? (float)(1 << FEW_SHIFT) : 1.f));
     }
 }
 
@@ -290,19 +327,6 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
 constexpr int WIDE_R = 4, WIDE_THREADS = 64 * WIDE_R;
 constexpr int wide_x_bytes(int tt) { return 32 * tt * GQ_COLS * 2; }     // of one block: 32 KB for 128 tokens
 constexpr int WIDE_A_ROW = 144, WIDE_A_BYTES = 16 * WIDE_A_ROW;      // dx: a wavefront's 16 rows x 64 columns; rows 16 bytes further apart than they are long, for the banks
-
-// Scaled weights of a word, exact in bfloat16.
-__device__ __forceinline__ gq_word4 weight_operand(uint32_t w, float s) {
-    gq_word4 v;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t bytes = h ? gq_high(w) : gq_low(w);
-        const gq_float2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(bytes, 512.f, true);
-        v[2 * h] = __builtin_amdgcn_perm(__float_as_uint(s * a.y), __float_as_uint(s * a.x), 0x07060302u);
-        v[2 * h + 1] = __builtin_amdgcn_perm(__float_as_uint(s * b.y), __float_as_uint(s * b.x), 0x07060302u);
-    }
-    return v;
-}
 
 // The other lane's of a pair.
 __device__ __forceinline__ float neighbour(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true)); }
@@ -741,7 +765,7 @@ skim_status launch_forward(skim_ctx *ctx, MmArgs A, int group, int x_type, void 
     if (groups > 0x7fffffff) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "%lld tokens on %lld rows are too many for one call", A.T, A.n);
     int nw = 4;
     while (nw < (nt == 1 ? 16 : 8) && groups * nw < 16ll * ctx->num_cu && nw < gq_col_blocks(A.m)) nw *= 2;
-    const size_t lds = (size_t)nw * MATS * rt * nt * 1024;
+    const size_t lds = (size_t)nw * MATS * (nt == 1 ? 16 * FEW_TOKEN * 4 : rt * nt * 1024);
     const int64_t octet = x_type == SKIM_BF16 ? 16 : 8, es = x_type == SKIM_BF16 ? 2 : 1;
     const bool vec = A.m % 8 == 0 && (A.ldx * es) % octet == 0 && (uintptr_t)A.x % octet == 0;
     with_group(group, [&](auto g) {

@@ -154,3 +154,52 @@ def test_rms_norm_scales_of_products_that_are_no_numbers(ctx, dtype, T, m):
     h[1, 7] = r[1, 7] = big
     o = ctx.rms_norm(h, pruned, residual=r)
     assert torch.isinf(o["h"][1, 7]) and no_number(o, 1) and same(o, ctx.rms_norm(x, pruned, residual=x), [t for t in range(T) if t != 1])
+
+
+# ---- values at the ends of the types' ranges --------------------------------------------------------------------------------
+
+def scaled_matrix(rng, n, m, group, power):
+    q, s = quantise(weights(rng, n, m) * np.float32(2.0) ** power, group)
+    codes, scales = pack(q, s, group)
+    return dict(codes=codes.cuda(), scales=scales.cuda(), n=n, m=m, group=group), dense(q, s, group)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 3, 17, 40, 64, 65, 130])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("power,of_x", [(-40, 124), (-100, 120), (110, -90), (125, -110), (-119, 40)])
+def test_products_of_large_and_small_values(ctx, T, group, power, of_x):
+    """Weights of 2^power / 50 and x of 2^of_x: every product and sum of the formula is far from the ends of float32, whatever its factors are, and so are the results of any
+    number of tokens.  (125: groups with an outlier have scales of 2^121.  2^-119 / 50 / 7 is above the least scale, 2^-126, for a group's largest weight; groups below it have codes of 0 or 1, as the format says.)"""
+    rng = np.random.default_rng(T + group)
+    n, m = 150, 700
+    gq, W = scaled_matrix(rng, n, m, group, power)
+    x = torch.from_numpy(rng.standard_normal((T, m))).to(BF16).double() * 2.0 ** of_x      # (exact: a power of two)
+    v = x.numpy()
+    want, size = v @ W.T, np.abs(v) @ np.abs(W).T
+    assert np.isfinite(want).all() and 2.0 ** -100 < np.abs(want).max() < 2.0 ** 100
+    y = ctx.group_matmul(gq, x.to(BF16).cuda(), out_dtype=torch.float32)
+    close(y, want, 2.0 ** -24 * np.abs(want) + loss(m) * size, "y")
+    tq, V = scaled_matrix(rng, m, n, group, power)
+    want, size = v @ V, np.abs(v) @ np.abs(V)
+    close(ctx.group_matmul_dx(tq, x.to(BF16).cuda(), out_dtype=torch.float32), want, 2.0 ** -24 * np.abs(want) + loss(m) * size, "dx")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 16, 33, 64, 65])
+def test_gated_block_of_large_activations_and_small_weights(ctx, T):
+    """g and u of about one from x of 2^122: q x alone, without its scale, is past the largest float32 from some four of them on."""
+    rng = np.random.default_rng(T)
+    n, m, group = 100, 600, 64
+    (gate, Wg), (up, Wu) = scaled_matrix(rng, n, m, group, -122), scaled_matrix(rng, n, m, group, -122)
+    x = torch.from_numpy(rng.standard_normal((T, m))).to(BF16).double() * 2.0 ** 122
+    xb, value = x.to(BF16).cuda(), x.numpy()
+    g, u, eg, eu = glu_errors(value, Wg, Wu, m)
+    want = silu(g) * u
+    a = ctx.group_glu(gate, up, xb, out_dtype=torch.float32)
+    close(a, want, 1.1 * eg * np.abs(u) + np.abs(silu(g)) * eu + 1.1 * eg * eu + (U[torch.float32] * 1.01 + (8 + np.minimum(np.abs(g), 100)) * 2.0 ** -24) * np.abs(want), "a")
+    da, dav = gradient(rng, T, n)
+    o = ctx.group_glu_backward(gate, up, xb, da, want_dx=False)
+    dg, du, eg, eu = gated_gradients(value, dav, Wg, Wu, m)
+    close(o["dgate"], dg, eg + U[BF16] * 1.01 * (np.abs(dg) + eg), "dgate")
+    close(o["dup"], du, eu + U[BF16] * 1.01 * (np.abs(du) + eu), "dup")
