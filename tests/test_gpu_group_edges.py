@@ -188,11 +188,11 @@ def test_products_of_large_and_small_values(ctx, T, group, power, of_x):
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 16, 33, 64, 65])
 def test_gated_block_of_large_activations_and_small_weights(ctx, T):
-    """g and u of about one from x of 2^122: q x alone, without its scale, is past the largest float32 from some four of them on."""
+    """g and u of a few units from x of 2^125 (and up to 2^127.3): sums of q x, without the scales, come past the largest float32."""
     rng = np.random.default_rng(T)
-    n, m, group = 100, 600, 64
+    n, m, group = 100, 600, 128
     (gate, Wg), (up, Wu) = scaled_matrix(rng, n, m, group, -122), scaled_matrix(rng, n, m, group, -122)
-    x = torch.from_numpy(rng.standard_normal((T, m))).to(BF16).double() * 2.0 ** 122
+    x = torch.from_numpy(rng.standard_normal((T, m))).to(BF16).double() * 2.0 ** 125
     xb, value = x.to(BF16).cuda(), x.numpy()
     g, u, eg, eu = glu_errors(value, Wg, Wu, m)
     want = silu(g) * u
