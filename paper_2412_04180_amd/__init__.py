@@ -484,11 +484,9 @@ class Context:
         assert x_scales.numel() == T, what
         return p, E4M3, ld, x_scales.data_ptr(), T
 
-    def _group_scratch(self, n, m, T, to_input):
+    def _group_scratch(self, n, m, T, gradients, x, x_type, ldx, dx_type=BF16):
         """(pointer, bytes, tensor) of the scratch of a product: it goes back to the allocator with this stream's work queued ahead of its next use."""
-        return self._scratch(self.lib.skim_group_scratch_bytes(self.h, n, m, T, to_input))
-
-    def _scratch(self, need):
+        need = self.lib.skim_group_scratch_bytes_for(self.h, n, m, T, gradients, x, x_type, ldx, dx_type)
         if need == 0:
             return None, 0, None
         scratch = self.empty((need,), self.torch.uint8)
@@ -527,7 +525,7 @@ class Context:
         xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_matmul: x")
         dtype, yt = self._result_type(out, out_dtype)
         y = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_matmul: out")
-        sp, sb, _keep = self._group_scratch(n, m, T, 0)
+        sp, sb, _keep = self._group_scratch(n, m, T, 0, xp, xt, ldx)
         self._check(self.lib.skim_group_matmul(self.h, codes, scales, n, m, group, xp, xt, ldx, xs, T, y.data_ptr(), yt, sp, sb))
         return y
 
@@ -537,7 +535,7 @@ class Context:
         dyp, ld, T = self._rows(dy, (self.torch.bfloat16,), n, "group_matmul_dx: dy")
         dtype, yt = self._result_type(out, out_dtype)
         dx = self._result(out, (m,) if dy.dim() == 1 else (T, m), dtype, "group_matmul_dx: out")
-        sp, sb, _keep = self._group_scratch(n, m, T, 1)
+        sp, sb, _keep = self._group_scratch(n, m, T, 1, dyp, BF16, ld)
         self._check(self.lib.skim_group_matmul_dx(self.h, codes, scales, n, m, group, dyp, ld, T, dx.data_ptr(), yt, sp, sb))
         return dx
 
@@ -549,7 +547,7 @@ class Context:
         xp, xt, ldx, xs, T = self._group_input(x, x_scales, m, "group_glu: x")
         dtype, yt = self._result_type(out, out_dtype)
         a = self._result(out, (n,) if x.dim() == 1 else (T, n), dtype, "group_glu: out")
-        sp, sb, _keep = self._group_scratch(n, m, T, 0)
+        sp, sb, _keep = self._group_scratch(n, m, T, 0, xp, xt, ldx)
         self._check(self.lib.skim_group_glu(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, a.data_ptr(), yt, sp, sb))
         return a
 
@@ -570,7 +568,7 @@ class Context:
         dup = self._result(out.get("dup"), lead + (n,), t.bfloat16, "group_glu_backward: dup")
         dtype, dt = self._result_type(out.get("dx"), out_dtype)
         dx = self._result(out.get("dx"), lead + (m,), dtype, "group_glu_backward: dx") if want_dx else None
-        sp, sb, _keep = self._scratch(self.lib.skim_group_scratch_bytes_for(self.h, n, m, T, 2 if want_dx else 0, xp, xt, ldx, dt))
+        sp, sb, _keep = self._group_scratch(n, m, T, 2 if want_dx else 0, xp, xt, ldx, dt)
         self._check(self.lib.skim_group_glu_backward(self.h, gc, gs, uc, us, n, m, group, xp, xt, ldx, xs, T, dap, ldda, dgate.data_ptr(),
                                                      dup.data_ptr(), None if dx is None else dx.data_ptr(), dt, sp, sb))
         return dict(dx=dx, dgate=dgate, dup=dup)

@@ -203,3 +203,43 @@ def test_gated_block_of_large_activations_and_small_weights(ctx, T):
     dg, du, eg, eu = gated_gradients(value, dav, Wg, Wu, m)
     close(o["dgate"], dg, eg + U[BF16] * 1.01 * (np.abs(dg) + eg), "dgate")
     close(o["dup"], du, eu + U[BF16] * 1.01 * (np.abs(du) + eu), "dup")
+
+
+# ---- scratch ----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+def test_scratch_holds_a_copy_of_x_only_where_the_tiles_take_one(ctx):
+    """The size for one call is that for any call less the copy, where rows lie on 16-byte borders; it is 0 for what the calls reject."""
+    lib, h = ctx.lib, ctx.h
+    of = lambda n, m, T, g, x, xt, ld, dt=1: lib.skim_group_scratch_bytes_for(h, n, m, T, g, x, xt, ld, dt)  # noqa: E731
+    any_call = lambda n, m, T, g: lib.skim_group_scratch_bytes(h, n, m, T, g)  # noqa: E731
+    copy = lambda columns, T: (-(-columns // 8) * 8 * T * 2 + 255) // 256 * 256  # noqa: E731
+    for n, m, T in ((4096, 11008, 2048), (11008, 4096, 131072), (300, 1000, 90), (1021, 2999, 70)):
+        as_it_is = m % 8 == 0
+        assert any_call(n, m, T, 0) - of(n, m, T, 0, 1 << 20, 1, m) == (copy(m, T) if as_it_is else 0)
+        assert any_call(n, m, T, 0) == of(n, m, T, 0, 1 << 20, 2, m) == of(n, m, T, 0, (1 << 20) + 2, 1, m) == of(n, m, T, 0, 1 << 20, 1, m + 1)
+        assert any_call(n, m, T, 1) - of(n, m, T, 1, 1 << 20, 1, n) == (copy(n, T) if n % 8 == 0 else 0)
+        assert any_call(n, m, T, 2) == of(n, m, T, 2, 1 << 20, 2, m) >= of(n, m, T, 2, 1 << 20, 1, m)
+        assert of(n, m, T, 2, 1 << 20, 2, m, 0) > 8 * n * T                              # (dgate and dup in 16 bits)
+    assert of(300, 1000, 64, 0, 1 << 20, 2, 1000) == 0 and of(300, 1000, 1, 1, 1 << 20, 1, 300) > 0
+    for bad in ((0, 8, 90, 0, 0, 1, 8), (8, 0, 90, 0, 0, 1, 8), (8, 8, 0, 0, 0, 1, 8), (8, 8, 90, 3, 0, 1, 8), (8, 8, 90, -1, 0, 1, 8), (8, 8, 90, 0, 0, 0, 8), (8, 8, 90, 0, 0, 3, 8),
+                (8, 16, 90, 0, 0, 2, 15), (16, 8, 90, 1, 0, 1, 15), (8, 8, 90, 1, 0, 2, 8), (8, 8, 90, 1, 0, 1, 8, 2), (8, 8, 90, 2, 0, 2, 8, 2), (1 << 24, 8, 90, 0, 0, 2, 8)):
+        assert of(*bad) == 0, bad
+
+
+@pytest.mark.gpu
+def test_long_prompts_allocate_their_results_and_no_copies(ctx):
+    rng = np.random.default_rng(2)
+    T, n, m = 16384, 256, 2048
+    gq, _ = matrix(rng, n, m, 128)
+    x = torch.zeros((T, m), dtype=BF16, device="cuda")
+    dy = torch.zeros((T, n), dtype=BF16, device="cuda")
+    for call, result in ((lambda: ctx.group_matmul(gq, x), 2 * T * n), (lambda: ctx.group_glu(gq, gq, x), 2 * T * n), (lambda: ctx.group_matmul_dx(gq, dy), 2 * T * m)):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        call()
+        # (partial sums of at most 32 MB; a copy of x would be 67 MB, of dy 8)
+        assert torch.cuda.max_memory_allocated() - before <= result + (32 << 20) + (1 << 20)
+        aligned = ctx.lib.skim_group_scratch_bytes_for(ctx.h, n, m, T, 0, x.data_ptr(), 1, m, 1)
+        assert torch.cuda.max_memory_allocated() - before <= result + max(aligned, ctx.lib.skim_group_scratch_bytes_for(ctx.h, n, m, T, 1, dy.data_ptr(), 1, n, 1)) + 4096
