@@ -243,3 +243,32 @@ def test_long_prompts_allocate_their_results_and_no_copies(ctx):
         assert torch.cuda.max_memory_allocated() - before <= result + (32 << 20) + (1 << 20)
         aligned = ctx.lib.skim_group_scratch_bytes_for(ctx.h, n, m, T, 0, x.data_ptr(), 1, m, 1)
         assert torch.cuda.max_memory_allocated() - before <= result + max(aligned, ctx.lib.skim_group_scratch_bytes_for(ctx.h, n, m, T, 1, dy.data_ptr(), 1, n, 1)) + 4096
+
+
+# ---- strides and alignment of the backward pass's inputs ------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 16, 40, 64, 65, 130])
+@pytest.mark.parametrize("n", [96, 101, 200])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (8, 0), (4, 4), (4, 2), (5, 3), (0, 1)])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_glu_backward_with_rows_of_any_stride(ctx, T, n, pad, offset, kind):
+    """da and x on rows further apart than they are long (NaNs between them) and off every border, each with fours and octets on theirs and not."""
+    rng = np.random.default_rng(T * 100 + n + 10 * pad + offset)
+    m, group = 264, 64
+    (gate, Wg), (up, Wu) = matrix(rng, n, m, group), matrix(rng, n, m, group)
+    x, s, value = inputs(rng, T, m, kind, m + pad, offset)
+    da, _, dav = inputs(rng, T, n, "bf16", n + pad, offset)
+    dg, du, eg, eu = gated_gradients(value, dav, Wg, Wu, m)
+    u = U[BF16] * 1.01
+    want, size = dg @ Wg + du @ Wu, np.abs(dg) @ np.abs(Wg) + np.abs(du) @ np.abs(Wu)
+    off = (eg + 2.0 ** -16 * np.abs(dg)) @ np.abs(Wg) + (eu + 2.0 ** -16 * np.abs(du)) @ np.abs(Wu) + loss(4 * n) * 1.01 * size
+    o = ctx.group_glu_backward(gate, up, x, da, x_scales=s, out_dtype=torch.float32)
+    close(o["dgate"], dg, eg + u * (np.abs(dg) + eg), "dgate")
+    close(o["dup"], du, eu + u * (np.abs(du) + eu), "dup")
+    close(o["dx"], want, 1.01 * off + 2.0 ** -24 * np.abs(want), "dx")
+    o = ctx.group_glu_backward(gate, up, x, da, x_scales=s)
+    sg, su = o["dgate"].cpu().double().numpy(), o["dup"].cpu().double().numpy()
+    if T > 64:
+        want, off = sg @ Wg + su @ Wu, loss(4 * n) * 1.01 * (np.abs(sg) @ np.abs(Wg) + np.abs(su) @ np.abs(Wu))
+    close(o["dx"], want, u * (np.abs(want) + off) + 1.01 * off, "dx in bfloat16")
