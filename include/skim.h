@@ -99,7 +99,8 @@ skim_status skim_set_workspace(skim_ctx *ctx, void *dev_ptr, size_t bytes);
  * bounds).  With validation on, each such call first runs one pass over W, S
  * and alpha, waits for it (the call synchronises with the stream), and returns
  * SKIM_ERR_NONFINITE, with the text naming the array, before any other work.
- * Uses 256 bytes of the registered workspace. */
+ * Uses 256 bytes of the registered workspace.  skim_group_quantize then checks
+ * its W in the same way (finite, below 2^127 in size), without a workspace. */
 skim_status skim_validate_enable(skim_ctx *ctx, int on);
 
 /* Optional timing of the two phases of a clustering call (skim_error_table,
@@ -301,7 +302,8 @@ typedef enum { SKIM_F32 = 0, SKIM_BF16 = 1, SKIM_E4M3 = 2 } skim_dtype;
  *   0 past the matrix.
  * The sizes are -1 for arguments that the calls reject.  n, m <= SKIM_GROUP_MAX, fewer than 2^31 blocks.
  *
- * skim_group_quantize: W dev, n x m float32, stride ld; finite, and below 2^127 in size.
+ * skim_group_quantize: W dev, n x m float32, stride ld; finite, and below 2^127 in size (looked for with skim_validate_enable; else the codes of a group
+ * with another value are unspecified).
  * skim_group_unpack: Wq dev float32 n x m, stride m. */
 #define SKIM_GROUP_MAX (1 << 23)
 int64_t skim_group_code_words(int64_t n, int64_t m);

@@ -203,8 +203,8 @@ class Context:
             self._check(self.lib.skim_set_workspace(self.h, _dp(self._ws), need))
 
     def validate_enable(self, on=True):
-        """Make the clustering calls check W, S and alpha first (they then synchronise and raise SkimError with
-        status SKIM_ERR_NONFINITE on a value the method is not defined on)."""
+        """Make the clustering calls check W, S and alpha first, and group_quantize its W (they then synchronise and raise SkimError
+        with status SKIM_ERR_NONFINITE on a value the method is not defined on)."""
         self._check(self.lib.skim_validate_enable(self.h, 1 if on else 0))
 
     def profile_enable(self, on=True):

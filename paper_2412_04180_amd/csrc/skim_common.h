@@ -27,8 +27,9 @@ struct skim_ctx {
     int validate;        // check W, S, alpha of the clustering calls for values the method is not defined on
     void *pack_scratch;  // this device's address of the static scratch of skim_pack_static
     int *sort_counters;  // device memory owned by the context: units of work handed out by the running sort_kernel, zero between
-                         // launches (whoever takes the last one clears it)
+                         // launches (whoever takes the last one clears it); word SKIM_GROUP_FLAG: what skim_group_quantize's validation found
 };
+constexpr int SKIM_GROUP_FLAG = 32;
 
 #define SKIM_FAIL(ctx, code, ...)                                   \
     do {                                                            \

@@ -2,6 +2,7 @@
 // are in skim_group_mm.hip.
 #include "skim_group.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -109,6 +110,29 @@ __global__ void __launch_bounds__(64 * GQ_WAVES) group_unpack_kernel(const uint3
     }
 }
 
+// Input validation (off unless the caller asks for it): 1 for a weight that is not finite, or of 2^127 and more.
+__global__ void group_validate_clear_kernel(int *flag) { *flag = 0; }
+__global__ void __launch_bounds__(256) group_validate_kernel(const float *__restrict__ W, long long n, long long m, long long ld, int *flag) {
+    int bad = 0;
+    for (long long row = blockIdx.x; row < n; row += gridDim.x)
+        for (long long j = threadIdx.x; j < m; j += 256)
+            if (!(fabsf(W[row * ld + j]) < 0x1p127f)) bad = 1;
+    if (bad) atomicOr(flag, 1);
+}
+skim_status validate_weights(skim_ctx *ctx, const float *W, int64_t n, int64_t m, int64_t ld) {
+    if (!ctx->validate) return SKIM_OK;
+    int *const on_device = ctx->sort_counters + SKIM_GROUP_FLAG;
+    hipLaunchKernelGGL(group_validate_clear_kernel, dim3(1), dim3(1), 0, ctx->stream, on_device);
+    hipLaunchKernelGGL(group_validate_kernel, dim3((unsigned)std::min<int64_t>(n, 8ll * ctx->num_cu)), dim3(256), 0, ctx->stream, W, (long long)n, (long long)m, (long long)ld,
+                       on_device);
+    SKIM_HIP(ctx, hipGetLastError());
+    int flag = 0;
+    SKIM_HIP(ctx, hipMemcpyAsync(&flag, on_device, sizeof(int), hipMemcpyDeviceToHost, ctx->stream));
+    SKIM_HIP(ctx, hipStreamSynchronize(ctx->stream));
+    if (flag) SKIM_FAIL(ctx, SKIM_ERR_NONFINITE, "skim_group_quantize: W holds a value that is not finite, or of 2^127 or more");
+    return SKIM_OK;
+}
+
 template <typename F>
 void with_group(int group, F &&f) {
     if (group == 32) f(std::integral_constant<int, 32>{});
@@ -146,6 +170,7 @@ extern "C" skim_status skim_group_quantize(skim_ctx *ctx, const float *W, int64_
     if ((st = skim_group_check(ctx, codes, scales_bf16, n, m, group, "skim_group_quantize")) != SKIM_OK) return st;
     if (!W) SKIM_FAIL(ctx, SKIM_ERR_ARG, "skim_group_quantize: W must not be NULL");
     if (ld < m) SKIM_FAIL(ctx, SKIM_ERR_SHAPE, "skim_group_quantize: ld=%lld is less than m=%lld", (long long)ld, (long long)m);
+    if ((st = validate_weights(ctx, W, n, m, ld)) != SKIM_OK) return st;
     const long long nblocks = gq_row_blocks(n) * gq_col_blocks(m);
     const bool vec = m % 8 == 0 && ld % 4 == 0 && ((uintptr_t)W & 15) == 0;
     with_group(group, [&](auto g) {

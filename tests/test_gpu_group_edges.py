@@ -272,3 +272,36 @@ def test_glu_backward_with_rows_of_any_stride(ctx, T, n, pad, offset, kind):
     if T > 64:
         want, off = sg @ Wg + su @ Wu, loss(4 * n) * 1.01 * (np.abs(sg) @ np.abs(Wg) + np.abs(su) @ np.abs(Wu))
     close(o["dx"], want, u * (np.abs(want) + off) + 1.01 * off, "dx in bfloat16")
+
+
+# ---- input validation -----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,m,pad", [(1, 1, 0), (37, 300, 0), (5000, 256, 0), (40, 129, 3)])
+def test_validation_mode_reports_weights_that_have_no_code(gpu_lib, n, m, pad):
+    rng = np.random.default_rng(n)
+    store = torch.full((n, m + pad), float("nan"), device="cuda")           # (NaNs between the rows are nobody's)
+    W = store[:, :m]
+    W.copy_(torch.from_numpy(weights(rng, n, m)))
+    c = gpu_lib.Context(0)
+    try:
+        ref = c.group_quantize(W)
+        c.validate_enable(True)
+        for i, j in ((0, 0), (n // 2, m // 2), (n - 1, m - 1)):
+            kept = W[i, j].item()
+            for bad in (float("nan"), float("inf"), float("-inf"), 2.0 ** 127, -2.0 ** 127):
+                W[i, j] = bad
+                with pytest.raises(gpu_lib.SkimError, match="W holds") as e:
+                    c.group_quantize(W)
+                assert e.value.status == -6
+            W[i, j] = 1.5 * 2.0 ** 126
+            c.group_quantize(W)
+            W[i, j] = kept
+        got = c.group_quantize(W)
+        assert torch.equal(got["codes"], ref["codes"]) and torch.equal(got["scales"].view(torch.int16), ref["scales"].view(torch.int16))
+        c.validate_enable(False)
+        W[0, 0] = float("nan")
+        c.group_quantize(W)                                                 # off (the default): not looked for, no error
+        torch.cuda.synchronize()
+    finally:
+        c.close()
