@@ -630,10 +630,11 @@ void with_group(int group, F &&f) {
     else f(std::integral_constant<int, 128>{});
 }
 
-// Forward, tiles from so many tokens on.  us on up to 64 tokens, few / tiles: 4096 x 4096 16 tokens 9.1 / 15.7, 64 11.4 / 17.8; 4096 x 11008 16 14.8 /
-// 21.5, 64 25.4 / 24.3; gated 11008 x 4096 16 18 / 29, 64 36 / 32, from e4m3 34 / 34; beyond 64 each chunk of 32 tokens reads all codes once more.
+// Forward, tiles from so many tokens on.  The few-token kernel reads all codes once for every 32 tokens, the tiles once for 128, with a launch or two more and scratch.
+// us, few / tiles: 4096 x 4096 17 tokens 9.8 / 19.2, 64 11.6 / 21.1; 4096 x 11008 17 17 / 25, 64 25.2 / 27.5; gated 11008 x 4096 17 19.6 / 38, 64 33 / 39.5, from e4m3
+// 34 / 42.  Beyond 64: 4096 x 11008 65 46 / 28; gated 11008 x 4096 65 40 / 41, 96 51 / 42; on small matrices the tiles are behind for longer (1021 x 2999 65 12 / 20, 128
+// 12 / 21; 4096 x 4096 65 19.5 / 23.5), where a border that goes by their size would gain.
 constexpr int64_t WIDE_FROM = 65;
-
 
 bool all_on(int64_t border, std::initializer_list<const void *> ps) {
     for (const void *p : ps)
@@ -657,6 +658,7 @@ struct WidePlan {
 };
 WidePlan wide_plan(const skim_ctx *ctx, int64_t out, int64_t per, int64_t blocks, int64_t T) {
     WidePlan p;
+    static_assert(WIDE_FROM > 64, "forward tiles are of 128 tokens only, and so are the partial sums they write");
     p.tt = T <= 64 ? 2 : 4;
     p.ttiles = (T + 32 * p.tt - 1) / (32 * p.tt);
     const int64_t cu = ctx->num_cu, tiles = (out + per - 1) / per * p.ttiles, left = tiles % (2 * cu);
