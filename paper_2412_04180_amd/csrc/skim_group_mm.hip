@@ -934,6 +934,10 @@ extern "C" skim_status skim_group_glu_backward(skim_ctx *ctx, const uint32_t *ga
         scratch = (char *)scratch + pieces;
         scratch_bytes -= pieces;
     }
+    // (refused before anything is written: rows of dgate and dup that the tiles cannot copy need one of their own)
+    if (dx && !A.pieces && n % 8 && 2 * widened_bytes(n, T) > scratch_bytes)
+        SKIM_FAIL(ctx, SKIM_ERR_WORKSPACE, "%s: dx of %lld tokens on %lld rows needs %zu bytes of scratch, %zu given", who, (long long)T, (long long)n, 2 * widened_bytes(n, T),
+                  scratch_bytes);
     if ((st = launch_forward<MM_GLU_BACK>(ctx, A, group, x_type, scratch, scratch_bytes)) != SKIM_OK || !dx) return st;
     A.x = dgate_bf16, A.x2 = dup_bf16, A.ldx = n, A.x_scales = nullptr, A.y = dx, A.y_f32 = dx_type == SKIM_F32;
     if (A.pieces) A.x = A.pieces, A.x2 = A.pieces + 2 * T * A.ldp, A.ldx = A.ldp, A.T = 2 * T, A.paired = true;

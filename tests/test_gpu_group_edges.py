@@ -305,3 +305,24 @@ def test_validation_mode_reports_weights_that_have_no_code(gpu_lib, n, m, pad):
         torch.cuda.synchronize()
     finally:
         c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 70])
+def test_refused_gradients_leave_their_outputs_alone(ctx, T):
+    """Without scratch, dx of rows that are no multiple of 8 is refused, and dgate and dup are not written either."""
+    rng = np.random.default_rng(T)
+    n, m, group = 101, 264, 64
+    (gate, _), (up, _) = matrix(rng, n, m, group), matrix(rng, n, m, group)
+    x, _, _ = inputs(rng, T, m, "bf16")
+    da, _ = gradient(rng, T, n)
+    outs = [torch.full((T, k), 7.0, dtype=BF16, device="cuda") for k in (n, n, m)]
+    mats = [gate["codes"].data_ptr(), gate["scales"].data_ptr(), up["codes"].data_ptr(), up["scales"].data_ptr(), n, m, group]
+    call = lambda dx, scratch, room: ctx.lib.skim_group_glu_backward(ctx.h, *mats, x.data_ptr(), 1, m, None, T, da.data_ptr(), n, outs[0].data_ptr(), outs[1].data_ptr(),  # noqa: E731
+                                                                     dx, 1, scratch, room)
+    assert call(outs[2].data_ptr(), None, 0) == -4 and b"scratch" in ctx.lib.skim_last_error(ctx.h)
+    torch.cuda.synchronize()
+    assert all((o == 7).all() for o in outs)
+    assert call(None, None, 0) == 0                                         # (without dx none is needed)
+    torch.cuda.synchronize()
+    assert not (outs[0] == 7).any() and (outs[2] == 7).all()
