@@ -16,6 +16,8 @@
 
 #include "skim_common.h"
 
+#include <type_traits>
+
 constexpr int GQ_ROWS = 16, GQ_COLS = 128;
 constexpr uint32_t GQ_MASK = 0x87878787u;
 
@@ -36,3 +38,11 @@ __device__ __forceinline__ uint32_t gq_high(uint32_t w) { return __builtin_amdgc
 skim_status skim_group_check(skim_ctx *ctx, const void *codes, const void *scales, int64_t n, int64_t m, int group, const char *who);
 
 __device__ __forceinline__ float gq_scale(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+// f with the group as a constant.
+template <typename F>
+static inline void with_group(int group, F &&f) {
+    if (group == 32) f(std::integral_constant<int, 32>{});
+    else if (group == 64) f(std::integral_constant<int, 64>{});
+    else f(std::integral_constant<int, 128>{});
+}

@@ -3,7 +3,6 @@
 #include "skim_group.h"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace {
 
@@ -131,13 +130,6 @@ skim_status validate_weights(skim_ctx *ctx, const float *W, int64_t n, int64_t m
     SKIM_HIP(ctx, hipStreamSynchronize(ctx->stream));
     if (flag) SKIM_FAIL(ctx, SKIM_ERR_NONFINITE, "skim_group_quantize: W holds a value that is not finite, or of 2^127 or more");
     return SKIM_OK;
-}
-
-template <typename F>
-void with_group(int group, F &&f) {
-    if (group == 32) f(std::integral_constant<int, 32>{});
-    else if (group == 64) f(std::integral_constant<int, 64>{});
-    else f(std::integral_constant<int, 128>{});
 }
 
 }  // namespace

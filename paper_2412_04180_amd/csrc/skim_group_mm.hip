@@ -623,13 +623,6 @@ __global__ void __launch_bounds__(256) group_widen_kernel(const void *x, long lo
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
-template <typename F>
-void with_group(int group, F &&f) {
-    if (group == 32) f(std::integral_constant<int, 32>{});
-    else if (group == 64) f(std::integral_constant<int, 64>{});
-    else f(std::integral_constant<int, 128>{});
-}
-
 // Forward, tiles from so many tokens on.  The few-token kernel reads all codes once for every 32 tokens, the tiles once for 128, with a launch or two more and scratch.
 // us, few / tiles: 4096 x 4096 17 tokens 9.8 / 19.2, 64 11.6 / 21.1; 4096 x 11008 17 17 / 25, 64 25.2 / 27.5; gated 11008 x 4096 17 19.6 / 38, 64 33 / 39.5, from e4m3
 // 34 / 42.  Beyond 64: 4096 x 11008 65 46 / 28; gated 11008 x 4096 65 40 / 41, 96 51 / 42; on small matrices the tiles are behind for longer (1021 x 2999 65 12 / 20, 128
