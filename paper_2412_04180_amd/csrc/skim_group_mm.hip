@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(256) group_join_kernel(MmArgs A, int ttiles, i
 }
 
 // x as the tiles take it: bfloat16, rows of `columns` values on 16-byte borders.  (In the tiles themselves the conversion of e4m3 through registers
-// cost 40 % of their time, for want of registers; this pass, bound by the 3 bytes a value, costs 3 % of it on 512 tokens of 4096 values.)
+// cost 40 % of their time, for want of registers; this pass, bound by the 3 bytes a value, costs 3 to 5 % of it on 512 tokens of 4096 values.)
 template <int XT>
 __global__ void __launch_bounds__(256) group_widen_kernel(const void *x, long long ldx, long long T, int m, int columns, uint16_t *out) {
     const long long octets = columns / 8, at = (long long)blockIdx.x * 256 + threadIdx.x;
