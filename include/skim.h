@@ -318,7 +318,7 @@ skim_status skim_group_unpack(skim_ctx *ctx, const uint32_t *codes, const uint16
  * x: dev, SKIM_BF16 with x_scales NULL, or SKIM_E4M3 with x_scales dev float32[T]: token t is x_scales[t] times its row of x (what
  * skim_rms_norm writes).  Row strides ldx >= m, lddy >= n in elements; any alignment, but rows on 16-byte borders (8-byte ones for
  * e4m3) whose length is a multiple of 8 are read faster.  Results: SKIM_BF16 or SKIM_F32, dense, apart from all inputs.
- * Operands are exact and sums float32; a result is rounded once, to its type.  What x holds behind a row's m columns is not used.
+ * Operands are exact and sums float32 (from e4m3 of the 8-bit values, times the token's scale at the end); a result is rounded once, to its type.  What x holds behind a row's m columns is not used.
  * scratch (dev, 16-byte aligned; NULL with 0 bytes = none): skim_group_scratch_bytes(ctx, n, m, T, gradients) bytes, gradients = 0 for
  * skim_group_matmul and skim_group_glu, 1 for skim_group_matmul_dx, 2 for skim_group_glu_backward (n x m: the matrices; 0 for arguments that
  * the calls reject, and for up to 64 tokens forward).  It takes x in bfloat16 where rows come in e4m3 or off the 16-byte borders, without room for which

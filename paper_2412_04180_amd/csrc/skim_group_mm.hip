@@ -189,12 +189,12 @@ struct XOctet {
 // LDS in the order of the wavefronts.  Bound by the codes' way from memory: with up to 16 tokens a wavefront asks for U blocks at once, with their scales and
 // their columns of x, before it takes the first apart.  One token on 4096 x 11008 7.8 us (3.0 TB/s; 13.5 with a block at a time), gated on 11008 x 4096 12.6
 // (3.7 TB/s); in the 128 registers of its wavefronts is room for no more.
-// A scale s is a power of two times its significand in 1/2 .. 1.  Up to 16 tokens (LATE) codes enter the matrix cores times that power, which their conversion brings along
+// A scale s is a power of two times its significand, 1 to 2.  Up to 16 tokens (LATE) codes enter the matrix cores times that power, which their conversion brings along
 // for nothing, and a group's sum is multiplied by the significand once: no sum overflows that the formula's does not (sums of q x alone do, for x above 2^118), and
-// the power is 2^-8 of itself so that a scale of 2^124 finds room in the conversion's, exact down to the least scale (q 2^-133, a bfloat16).  x is the first operand there: a lane's
-// four sums are of one row then, and take one significand.  More tokens take weights times scales, as the tiles do.  us the one way / the other: one token on
-// 4096 x 11008 7.8 / 8.6, gated on 11008 x 4096 12.6 / 14.4; 32 tokens on 4096 x 11008 with groups of 32 29 / 25.5, gated 64 36 / 33.
-constexpr int FEW_SHIFT = 8;
+// none is smaller than a half of it.  (Powers are at most 2^118, where the conversion's own, 2^9 times that, ends; the rest of a larger scale goes with its significand.)
+// x is the first operand there: a lane's four sums are of one row then, and take one significand.  More tokens take weights times scales, as the tiles do.  us the one way
+// / the other: one token on 4096 x 11008 7.8 / 8.6, gated on 11008 x 4096 12.6 / 14.4; 32 tokens on 4096 x 11008 with groups of 32 29 / 25.5, gated 64 36 / 33.
+constexpr int FEW_POWER = 118;
 constexpr int FEW_TOKEN = 20;         // floats of a token's 16 rows in LDS: so that 64 lanes' of one access lie in different banks
 template <int XT, int NT, int G, int MODE, bool VEC>
 __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs A, int chunks) {
@@ -246,10 +246,10 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
 #pragma unroll
             for (int g = 0; g < GS; ++g) {
                 gq_float4 d[MATS] = {};
-                float power[MATS];
+                uint32_t power[MATS];                         // exponent field, in place
                 if constexpr (LATE) {
 #pragma unroll
-                    for (int a = 0; a < MATS; ++a) power[a] = ldexpf(1.f, __builtin_amdgcn_frexp_expf(gq_scale(s[u][a][0][g])) + 9 - FEW_SHIFT);
+                    for (int a = 0; a < MATS; ++a) power[a] = min(s[u][a][0][g] & 0x7F80u, (uint32_t)(FEW_POWER + 127) << 7);
                 }
 #pragma unroll
                 for (int k = g * (4 / GS); k < (g + 1) * (4 / GS); ++k) {
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
 #pragma unroll
                     for (int a = 0; a < MATS; ++a) {
                         if constexpr (LATE) {
-                            d[a] = mfma(b[0], code_operand(w[u][a][0][k], power[a]), d[a]);
+                            d[a] = mfma(b[0], code_operand(w[u][a][0][k], gq_scale(power[a] + (9u << 7))), d[a]);
                         } else {
 #pragma unroll
                             for (int r = 0; r < RT; ++r) {
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
                 if constexpr (LATE) {
 #pragma unroll
                     for (int a = 0; a < MATS; ++a) {
-                        const float f = __builtin_amdgcn_frexp_mantf(gq_scale(s[u][a][0][g]));
+                        const float f = gq_scale(s[u][a][0][g]) * gq_scale((254u << 7) - power[a]);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[a][0][0][i] = fmaf(f, d[a][i], acc[a][0][0][i]);
                     }
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(NT == 1 ? 1024 : 512) group_few_kernel(MmArgs 
             for (int w = 0; w < nw; ++w) v[a] += red[(w * MATS + a) * ROOM + at];
         const long long t = t0 + 16 * ((e >> 6) % NT) + (el & 15), rt = rt0 + (e >> 6) / NT;
         if (t < A.T)
-            finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], (XT == SKIM_E4M3 ? A.x_scales[t] : 1.f) * (LATE ? (float)(1 << FEW_SHIFT) : 1.f));
+            finish4<MODE>(A, t, rt * GQ_ROWS + 4 * (el >> 4), A.n, v[0], v[MATS - 1], XT == SKIM_E4M3 ? A.x_scales[t] : 1.f);
     }
 }
 

@@ -1,6 +1,5 @@
 """Products with 4-bit weights and the norm at the borders of what they are documented for: gradients in 16 bits, strides of every input, scratch of just
 the size that a call needs, values at the ends of the types' ranges.  Plain float64 on the CPU; U and loss() are derived in test_gpu_group.py."""
-import ctypes as C
 
 import numpy as np
 import pytest
@@ -167,9 +166,9 @@ def scaled_matrix(rng, n, m, group, power):
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 3, 17, 40, 64, 65, 130])
 @pytest.mark.parametrize("group", [32, 64, 128])
-@pytest.mark.parametrize("power,of_x", [(-40, 124), (-100, 120), (110, -90), (125, -110), (-119, 40)])
+@pytest.mark.parametrize("power,of_x", [(-40, 124), (-100, 120), (110, -90), (125, -110), (-119, 40), (-8, -112)])
 def test_products_of_large_and_small_values(ctx, T, group, power, of_x):
-    """Weights of 2^power / 50 and x of 2^of_x: every product and sum of the formula is far from the ends of float32, whatever its factors are, and so are the results of any
+    """Weights of 2^power / 50 and x of 2^of_x: every product and sum of the formula is a normal float32, whatever its factors are, and so are the results of any
     number of tokens.  (125: groups with an outlier have scales of 2^121.  2^-119 / 50 / 7 is above the least scale, 2^-126, for a group's largest weight; groups below it have codes of 0 or 1, as the format says.)"""
     rng = np.random.default_rng(T + group)
     n, m = 150, 700
@@ -177,7 +176,7 @@ def test_products_of_large_and_small_values(ctx, T, group, power, of_x):
     x = torch.from_numpy(rng.standard_normal((T, m))).to(BF16).double() * 2.0 ** of_x      # (exact: a power of two)
     v = x.numpy()
     want, size = v @ W.T, np.abs(v) @ np.abs(W).T
-    assert np.isfinite(want).all() and 2.0 ** -100 < np.abs(want).max() < 2.0 ** 100
+    assert np.isfinite(want).all() and 2.0 ** -122 < np.abs(want).max() < 2.0 ** 100
     y = ctx.group_matmul(gq, x.to(BF16).cuda(), out_dtype=torch.float32)
     close(y, want, 2.0 ** -24 * np.abs(want) + loss(m) * size, "y")
     tq, V = scaled_matrix(rng, m, n, group, power)
@@ -326,3 +325,18 @@ def test_refused_gradients_leave_their_outputs_alone(ctx, T):
     assert call(None, None, 0) == 0                                         # (without dx none is needed)
     torch.cuda.synchronize()
     assert not (outs[0] == 7).any() and (outs[2] == 7).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 16, 17, 64, 65])
+@pytest.mark.parametrize("of_x", [-120, 124])
+def test_scales_of_8_bit_activations_at_the_ends_of_float32(ctx, T, of_x):
+    """Sums are taken before the token's scale: it is multiplied on at the end, however large or small."""
+    rng = np.random.default_rng(T)
+    n, m, group = 100, 700, 64
+    gq, W = scaled_matrix(rng, n, m, group, 0 if of_x < 0 else -100)
+    q, s, value = inputs(rng, T, m, "e4m3")
+    s, value = s * 2.0 ** of_x, value * 2.0 ** of_x
+    assert torch.isfinite(s).all() and (s > 0).all()
+    want, size = value @ W.T, np.abs(value) @ np.abs(W).T
+    close(ctx.group_matmul(gq, q, x_scales=s, out_dtype=torch.float32), want, 2.0 ** -23 * np.abs(want) + loss(m) * size, "y")
