@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(64 * GQ_WAVES) group_quantize_kernel(const flo
     ((gq_word4 *)codes)[block * 64 + lane] = out;
 }
 
-// The dense matrix, bound by the 4 bytes written per weight: 11008 x 4096 in 35 us, 5.8 TB/s.
+// The dense matrix, bound by the 4 bytes written per weight: 11008 x 4096 in 35-40 us, 5.1-5.8 TB/s.
 template <int G, bool VEC>
 __global__ void __launch_bounds__(64 * GQ_WAVES) group_unpack_kernel(const uint32_t *__restrict__ codes, const uint16_t *__restrict__ scales, long long n,
                                                                      long long m, long long nblocks, float *__restrict__ Wq) {
